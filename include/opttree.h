@@ -42,6 +42,7 @@ extern "C" {
 
 #define OT_F32   0   /* IEEE binary32 */
 #define OT_BF16  1   /* bfloat16 */
+#define OT_E4M3  2   /* 8-bit float, pages of a paged cache only (ot_paged_cache) */
 
 /* limits of this build */
 #define OT_MAX_NODES     256   /* n  */
@@ -49,6 +50,7 @@ extern "C" {
 #define OT_MAX_DEPTH      32   /* d  */
 #define OT_MAX_HEAD_DIM  128
 #define OT_MAX_TREE_KEYS 8192     /* tree keys of the attention when they are more than the query rows */
+#define OT_MAX_APPEND    (1 << 24)  /* rows of a sequence that one call adds to a paged cache */
 #define OT_MASK_WORDS(n) (((n) + 63) / 64)
 
 OT_API int ot_version(void);                       /* 100*major + minor */
@@ -345,6 +347,121 @@ OT_API int ot_kv_append(const ot_attn_params* p, void* K_prefix, void* V_prefix,
                  const void* K_tree, const void* V_tree,
                  const int32_t* prefix_len, const int32_t* accept_len, const int32_t* accept_node,
                  int32_t* new_prefix_len, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Queries and keys of new tokens: norm of every head and position rotation in one pass, what stands between a layer's
+ * projections and ot_tree_verify_attention (whose Q and K arrive position-encoded).
+ *
+ * For sequence b, head h, token i (row x of head_dim values):
+ *   y_c = x_c / sqrt(mean_c(x_c^2) + eps) * weight[c]          (q_weight for Q, k_weight for K; NULL: y = x, no norm)
+ *   pos = first[b] + (offset ? offset[b][i] : i) + shift       (a draft tree: first = prefix lengths, offset = node depths,
+ *                                                               shift = -1, since the root is the last prefix row)
+ *   the pair (y_j, y_{j+R/2}), R = rotary_dim, or with `interleaved` (y_2j, y_2j+1), j < R/2, is turned by the angle
+ *   pos * inv_freq[j]:  (u cos - v sin, u sin + v cos);  columns from R on are not turned.
+ * Arithmetic in fp32, the angle, its sine and cosine in fp64 (a position of 10^6 leaves an fp32 angle two digits); one rounding at the end.
+ * Q_out / K_out may be Q / K themselves (same pointer and strides); otherwise outputs must not overlap inputs.
+ * Either of Q, K may be absent (q_heads / kv_heads = 0, its pointers ignored).  Infinities and NaNs stay in their own row.
+ * ---------------------------------------------------------------------- */
+typedef struct ot_qk_params {
+    int32_t batch, q_heads, kv_heads;   /* heads >= 0, not both 0 */
+    int32_t head_dim;                   /* 64 or 128 */
+    int32_t n;                          /* tokens per sequence, >= 1; batch * n < 2^31 */
+    int32_t dtype;                      /* OT_F32 | OT_BF16, of Q, K, the weights and the outputs */
+    int32_t rotary_dim;                 /* R: a multiple of 16, 0..head_dim */
+    int32_t interleaved;                /* 0: pairs (j, j + R/2); 1: pairs (2j, 2j + 1) */
+    int32_t shift;
+    float   eps;                        /* >= 0 */
+    int64_t q_strides[3], k_strides[3], qo_strides[3], ko_strides[3];   /* batch, head, token; elements, multiples of 16 bytes */
+} ot_qk_params;
+
+OT_API int ot_qk_norm_rope(const ot_qk_params* p, const void* Q, const void* K,
+                    const void* q_weight, const void* k_weight,     /* [head_dim], 16-byte aligned, or NULL */
+                    const double* inv_freq,                         /* [rotary_dim / 2]; may be NULL if rotary_dim == 0 */
+                    const int32_t* first,                           /* [batch] */
+                    const int32_t* offset,                          /* [batch][n] or NULL */
+                    void* Q_out, void* K_out, void* hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Paged K/V cache: a pool of pages of page_size rows for every KV head, and per sequence a table of the pages that hold
+ * its rows in order (row r of sequence b: row r % page_size of page page_table[b][r / page_size]).
+ *
+ * Element (page, h, r, c) is at pages + page*s[0] + h*s[1] + r*s[2] + c (strides in elements, multiples of 16 bytes).
+ * dtype OT_BF16: as they are.  dtype OT_E4M3: bytes of the OCP 8-bit format (as in ot_tree_verify_attention_fp8kv) with a
+ * scale for every page and head: byte q of page and head (page, h) stands for decode(q) * 2^(exp[page][h] - 127),
+ * exp in 1..253 (k_exp for keys, v_exp for values; other bytes are never written and stand for nothing in particular).
+ * A power of two costs no accuracy in a floating-point format, makes the widened value a bfloat16 without error, and lets
+ * a page's older rows follow a larger one by moving exponents.
+ * Table entries outside [0, num_pages) are no pages: nothing is read or written there (see the calls).
+ * ---------------------------------------------------------------------- */
+typedef struct ot_paged_cache {
+    int32_t num_pages, page_size;       /* page_size: 16, 32, 64, 128 or 256 */
+    int32_t kv_heads, head_dim;         /* head_dim 64 or 128 */
+    int32_t dtype;                      /* OT_BF16 | OT_E4M3 */
+    int32_t max_pages;                  /* entries per sequence in page_table; max_pages * page_size < 2^30 */
+    int64_t k_strides[3], v_strides[3]; /* page, head, row; elements */
+    void *k_pages, *v_pages;            /* device */
+    uint8_t *k_exp, *v_exp;             /* device [num_pages][kv_heads], OT_E4M3 only */
+    const int32_t* page_table;          /* device [batch][max_pages] */
+} ot_paged_cache;
+
+/* Rows join a paged cache: for j < count[b], row (rows ? rows[b][j] : j) of K and V becomes cache row cache_len[b] + j of
+ * every KV head.  With rotary_dim > 0 the key is turned on the way, by the angle of position cache_len[b] + j + shift
+ * (as in ot_qk_norm_rope); the stored value is rounded once, from fp32.
+ *   prompt or generated token: count = NULL (all n rows) or the lengths of padded prompts, rows = NULL
+ *   accepted branch:           count = accept_len, count_shift = -1, rows = accept_node (ot_verify_greedy / _sample)
+ * OT_E4M3: the exponent of a page and head becomes the smallest with which no new row of this call in it exceeds 448; if the page
+ * holds older rows of the sequence (those before cache_len[b]) it does not fall below what it was, and where it rises
+ * the older rows are rounded again at the new one.  Infinities are stored as +-448 at the exponent of the finite values,
+ * NaNs as NaN.
+ * cache_len[b] is clamped to [0, capacity], capacity = max_pages * page_size; count[b] + count_shift to [0, n].  Rows beyond
+ * the capacity, and all rows from the first table entry (at or after the page of row cache_len[b]) that is no page, are
+ * dropped; new_len[b] = cache_len[b] + rows stored.  A row index outside [0, n) stores a row of zeros.  Rows behind the new
+ * ones keep their bytes.  Pages that receive rows must not be shared by two sequences of the call or appear
+ * twice among a sequence's pages that do; K and V must not overlap the pool.  new_len must not overlap cache_len, count or rows. */
+typedef struct ot_append_params {
+    int32_t batch, n;                   /* 1..OT_MAX_APPEND rows per sequence in K and V; batch * n < 2^31 */
+    int32_t dtype;                      /* OT_F32 | OT_BF16, of K and V */
+    int32_t rotary_dim, interleaved, shift, count_shift;
+    int64_t k_strides[3], v_strides[3]; /* batch, head, row; elements, multiples of 16 bytes */
+} ot_append_params;
+
+OT_API int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* cache, const void* K, const void* V,
+                       const double* inv_freq,          /* [rotary_dim / 2]; may be NULL if rotary_dim == 0 */
+                       const int32_t* cache_len,        /* [batch] */
+                       const int32_t* count,            /* [batch] or NULL */
+                       const int32_t* rows,             /* [batch][n] or NULL */
+                       int32_t* new_len, void* hip_stream);
+
+/* Tree-masked attention over a paged cache (Algorithm 2's forward, and with tree_keys = 0 plain decoding): as
+ * ot_tree_verify_attention, with the prefix rows taken through the page table.  Q, O, K_tree and V_tree are bf16, also over an E4M3 cache:
+ * the tree's keys are not in the cache yet.
+ *   O[b,h,i,:] = sum_j softmax_j(scale * Q[b,h,i,:] . K[b,h/g,j,:]) V[b,h/g,j,:],  j over cache rows 0..prefix_len[b]-1 and the
+ *   tree rows j with bit j of mask[b][i];  a query that sees nothing yields zeros.
+ * Cache rows from prefix_len[b] on and tree rows that no query of their sequence sees may hold anything, infinities and NaNs
+ * included; tree rows that some query sees must be finite.  |scale * log2(e) * Q.K| stays below 2^31.
+ * prefix_len[b] is clamped to [0, max_pages * page_size] and rows of table entries that are no pages are left out (not seen
+ * by any query); both are reported in the status word of the workspace (OT_ATTN_STATUS_PREFIX_CLAMPED,
+ * OT_ATTN_STATUS_BAD_PAGE at OT_ATTN_STATUS_OFFSET; api: attn_status).
+ * The workspace is prepared once by ot_paged_attn_workspace_prepare, which zeroes its first OT_PAGED_SYNC_BYTES; every completed
+ * call leaves them as it found them but for the status word.  One workspace serves calls that follow one another on a
+ * stream (any sizes that fit it); calls that may overlap need one each. */
+#define OT_PAGED_SYNC_BYTES 65536
+#define OT_ATTN_STATUS_BAD_PAGE 2u
+typedef struct ot_paged_attn_params {
+    int32_t batch, q_heads;             /* q_heads % cache.kv_heads == 0 */
+    int32_t n;                          /* query rows, 1..OT_MAX_NODES */
+    int32_t tree_keys;                  /* rows of K_tree / V_tree, 0..OT_MAX_TREE_KEYS; 0: no tree (K_tree, V_tree, mask ignored) */
+    float   softmax_scale;              /* 0 => 1/sqrt(head_dim) */
+    int64_t q_strides[3], kt_strides[3], vt_strides[3], o_strides[3];
+} ot_paged_attn_params;
+
+OT_API size_t ot_paged_attn_workspace_bytes(const ot_paged_attn_params* p, const ot_paged_cache* cache);   /* 0 if invalid */
+OT_API int ot_paged_attn_workspace_prepare(void* workspace, size_t workspace_bytes, void* hip_stream);
+OT_API int ot_tree_verify_attention_paged(const ot_paged_attn_params* p, const ot_paged_cache* cache, const void* Q,
+                                   const void* K_tree, const void* V_tree,
+                                   const int32_t* prefix_len,    /* [batch] */
+                                   const uint64_t* mask,         /* [batch][n][OT_MASK_WORDS(tree_keys)] */
+                                   void* O, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------------
  * Yardsticks for the measurement (for callers that rate the kernels above against what this GPU reaches,

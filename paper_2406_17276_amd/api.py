@@ -15,7 +15,7 @@ import ctypes as C
 import os
 from dataclasses import dataclass
 
-OT_F32, OT_BF16 = 0, 1
+OT_F32, OT_BF16, OT_E4M3 = 0, 1, 2
 OT_MAX_NODES, OT_MAX_TOPK, OT_MAX_DEPTH = 256, 16, 32
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libopttree.so")
@@ -54,6 +54,31 @@ class AttnParams(C.Structure):
 class VerifyParams(C.Structure):
     _fields_ = [("batch", C.c_int32), ("vocab", C.c_int32), ("n", C.c_int32), ("logits_dtype", C.c_int32),
                 ("stride_seq", C.c_int64), ("stride_row", C.c_int64)]
+
+
+class QkParams(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("n", C.c_int32),
+                ("dtype", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("shift", C.c_int32), ("eps", C.c_float),
+                ("q_strides", C.c_int64 * 3), ("k_strides", C.c_int64 * 3), ("qo_strides", C.c_int64 * 3),
+                ("ko_strides", C.c_int64 * 3)]
+
+
+class PagedCacheParams(C.Structure):
+    _fields_ = [("num_pages", C.c_int32), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("dtype", C.c_int32), ("max_pages", C.c_int32), ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("page_table", C.c_void_p)]
+
+
+class AppendParams(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("n", C.c_int32), ("dtype", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("shift", C.c_int32), ("count_shift", C.c_int32), ("k_strides", C.c_int64 * 3), ("v_strides", C.c_int64 * 3)]
+
+
+class PagedAttnParams(C.Structure):
+    _fields_ = [("batch", C.c_int32), ("q_heads", C.c_int32), ("n", C.c_int32), ("tree_keys", C.c_int32),
+                ("softmax_scale", C.c_float), ("q_strides", C.c_int64 * 3), ("kt_strides", C.c_int64 * 3),
+                ("vt_strides", C.c_int64 * 3), ("o_strides", C.c_int64 * 3)]
 
 
 def lib():
@@ -127,6 +152,17 @@ def lib():
         L.ot_tree_verify_attention_timed.restype = C.c_int
         L.ot_tree_verify_attention_timed.argtypes = ([C.POINTER(AttnParams)] + [C.c_void_p] * 9 +
                                                      [C.c_size_t, C.c_void_p, C.c_void_p, C.c_void_p])
+        L.ot_qk_norm_rope.restype = C.c_int
+        L.ot_qk_norm_rope.argtypes = [C.POINTER(QkParams)] + [C.c_void_p] * 10
+        L.ot_kv_append_paged.restype = C.c_int
+        L.ot_kv_append_paged.argtypes = [C.POINTER(AppendParams), C.POINTER(PagedCacheParams)] + [C.c_void_p] * 8
+        L.ot_paged_attn_workspace_bytes.restype = C.c_size_t
+        L.ot_paged_attn_workspace_bytes.argtypes = [C.POINTER(PagedAttnParams), C.POINTER(PagedCacheParams)]
+        L.ot_paged_attn_workspace_prepare.restype = C.c_int
+        L.ot_paged_attn_workspace_prepare.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p]
+        L.ot_tree_verify_attention_paged.restype = C.c_int
+        L.ot_tree_verify_attention_paged.argtypes = ([C.POINTER(PagedAttnParams), C.POINTER(PagedCacheParams)] + [C.c_void_p] * 7 +
+                                                     [C.c_size_t, C.c_void_p])
         _lib = L
     return _lib
 
@@ -310,10 +346,12 @@ def attn_workspace(p: AttnParams, device):
 
 OT_ATTN_STATUS_OFFSET = 4092
 OT_ATTN_STATUS_PREFIX_CLAMPED = 1
+OT_ATTN_STATUS_BAD_PAGE = 2
 
 
 def attn_status(workspace) -> int:
-    """The status word the attention calls keep in their workspace (bit 0: a prefix length was clamped).
+    """The status word the attention calls keep in their workspace (bit 0: a prefix length was clamped; bit 1, paged cache: rows of
+    a table entry that is no page were left out).
     Reads device memory: synchronises the current stream."""
     import torch
     return int(workspace[OT_ATTN_STATUS_OFFSET:OT_ATTN_STATUS_OFFSET + 4].view(torch.int32).item())
@@ -384,6 +422,97 @@ def kv_append(K_prefix, V_prefix, K_tree, V_tree, prefix_len, accept_len, accept
     if st:
         raise OptTreeError(st, "ot_kv_append")
     return new_len
+
+
+# ---------------------------------------------------------------------------
+# Operators around a paged cache
+# ---------------------------------------------------------------------------
+@dataclass
+class PagedCache:
+    """ot_paged_cache: a pool of pages and the sequences' page tables.  k, v [pages, Hkv, page_size, D] (any strides of 16
+    bytes, last dimension contiguous): bfloat16, or uint8 / float8_e4m3fn bytes with exponents k_exp, v_exp uint8
+    [pages, Hkv]; table int32 [B, max_pages]."""
+    k: "object"
+    v: "object"
+    table: "object"
+    k_exp: "object" = None
+    v_exp: "object" = None
+
+
+def alloc_paged_cache(num_pages: int, kv_heads: int, page_size: int, head_dim: int, batch: int, max_pages: int, eight_bit: bool = True,
+                      device="cuda") -> PagedCache:
+    """An empty cache; its table's entries are -1 (no page) until the caller hands pages out."""
+    import torch
+    shape = (num_pages, kv_heads, page_size, head_dim)
+    table = torch.full((batch, max_pages), -1, dtype=torch.int32, device=device)
+    if not eight_bit:
+        return PagedCache(torch.empty(shape, dtype=torch.bfloat16, device=device), torch.empty(shape, dtype=torch.bfloat16, device=device), table)
+    one = lambda: torch.full(shape[:2], 127, dtype=torch.uint8, device=device)
+    return PagedCache(torch.empty(shape, dtype=torch.uint8, device=device), torch.empty(shape, dtype=torch.uint8, device=device), table,
+                      one(), one())
+
+
+def qk_norm_rope(Q, K, first, inv_freq=None, offset=None, shift: int = 0, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 interleaved: bool = False, q_out=None, k_out=None):
+    """ot_qk_norm_rope on the current stream.  Q [B,Hq,n,D], K [B,Hkv,n,D] (either may be None); first int32 [B]; inv_freq float64
+    [rotary_dim / 2] or None; offset int32 [B,n] or None (0, 1, ..); weights [D] or None (no norm).  Returns (Q_out, K_out)."""
+    st, q, k = (_binding or _native()).qk_norm_rope(Q, K, q_weight, k_weight, inv_freq, first, offset, shift, eps, interleaved, q_out,
+                                                    k_out)
+    if st:
+        raise OptTreeError(st, "ot_qk_norm_rope")
+    return q, k
+
+
+def kv_append_paged(cache: PagedCache, K, V, cache_len, count=None, rows=None, count_shift: int = 0, inv_freq=None, shift: int = 0,
+                    interleaved: bool = False, new_len=None):
+    """ot_kv_append_paged on the current stream.  K, V [B,Hkv,n,D]; cache_len, count int32 [B]; rows int32 [B,n]; inv_freq float64
+    [rotary_dim / 2] turns the keys on the way.  Returns the new lengths (int32 [B])."""
+    st, new = (_binding or _native()).kv_append_paged(K, V, cache.k, cache.v, cache.k_exp, cache.v_exp, cache.table, cache_len, count,
+                                                      rows, count_shift, inv_freq, shift, interleaved, new_len)
+    if st:
+        raise OptTreeError(st, "ot_kv_append_paged")
+    return new
+
+
+def paged_params(Q, cache: PagedCache, K_tree=None, V_tree=None, softmax_scale: float = 0.0):
+    """The C structs of an attention call (size queries, measurement, callers of the C ABI)."""
+    st = lambda t: (C.c_int64 * 3)(*(t.stride()[:3] if t is not None else (0, 0, 0)))
+    V_tree = K_tree if V_tree is None else V_tree
+    p = PagedAttnParams(Q.shape[0], Q.shape[1], Q.shape[2], 0 if K_tree is None else K_tree.shape[2], float(softmax_scale), st(Q),
+                        st(K_tree), st(V_tree), st(Q))
+    ptr = lambda t: None if t is None else t.data_ptr()
+    P, H, ps, D = cache.k.shape
+    c = PagedCacheParams(P, ps, H, D, OT_BF16 if cache.k_exp is None else OT_E4M3, cache.table.shape[1], st(cache.k), st(cache.v),
+                         ptr(cache.k), ptr(cache.v), ptr(cache.k_exp), ptr(cache.v_exp), ptr(cache.table))
+    return p, c
+
+
+def paged_attn_workspace(Q, cache: PagedCache, K_tree=None):
+    """A workspace for tree_verify_attention_paged, already prepared (ot_paged_attn_workspace_prepare)."""
+    import torch
+    p, c = paged_params(Q, cache, K_tree)
+    need = int(lib().ot_paged_attn_workspace_bytes(C.byref(p), C.byref(c)))
+    if need == 0:
+        raise OptTreeError(-2, "ot_paged_attn_workspace_bytes")
+    with torch.cuda.device(Q.device):
+        ws = torch.empty(need, dtype=torch.uint8, device=Q.device)
+        _check(lib().ot_paged_attn_workspace_prepare(ws.data_ptr(), ws.numel(), _stream()), "ot_paged_attn_workspace_prepare")
+        torch.cuda.current_stream().synchronize()      # the workspace may be used on any stream afterwards
+    return ws
+
+
+def tree_verify_attention_paged(Q, cache: PagedCache, prefix_len, K_tree=None, V_tree=None, mask=None, out=None, workspace=None,
+                                softmax_scale: float = 0.0):
+    """ot_tree_verify_attention_paged on the current stream.  Q bf16 [B,Hq,n,D]; prefix_len int32 [B]; K_tree, V_tree bf16
+    [B,Hkv,keys,D] with mask int64 [B,n,ceil(keys/64)], or None (plain decoding).  A caller-supplied workspace must be a
+    prepared one (paged_attn_workspace)."""
+    if workspace is None:
+        workspace = paged_attn_workspace(Q, cache, K_tree)
+    st, o = (_binding or _native()).attention_paged(Q, cache.k, cache.v, cache.k_exp, cache.v_exp, cache.table, K_tree, V_tree, prefix_len,
+                                                    mask, out, workspace, softmax_scale)
+    if st:
+        raise OptTreeError(st, "ot_tree_verify_attention_paged")
+    return o
 
 
 # ---------------------------------------------------------------------------

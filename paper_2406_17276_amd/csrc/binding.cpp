@@ -13,6 +13,7 @@
 #include <ATen/ATen.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Device.h>
 #include <torch/csrc/Exceptions.h>
@@ -433,6 +434,178 @@ PyObject* kv_append(PyObject* const* a, Py_ssize_t na) {
     return Py_BuildValue("iO", st, o.p);
 }
 
+// ---- operators around a paged cache ----------------------------------------------------------------------------------
+// All tensors of a call are on one GPU, which is made current for the call, on that GPU's current torch stream.
+struct OnDevice {
+    const at::Device dev;
+    const c10::DeviceGuard guard;
+    explicit OnDevice(const at::Tensor& t) : dev(t.device()), guard(checked(t)) {}
+    static at::Device checked(const at::Tensor& t) {
+        if (!t.is_cuda()) fail(PyExc_ValueError, "tensors must be on a GPU");
+        return t.device();
+    }
+    void* stream() const { return (void*)c10::hip::getCurrentHIPStream(dev.index()).stream(); }
+    void check(const at::Tensor& t, const char* name) const {
+        if (t.device() != dev) fail(PyExc_ValueError, "%s is on another device", name);
+    }
+};
+// a contiguous helper array of the given type and shape (sizes < 0: any)
+const at::Tensor* array(PyObject* o, const OnDevice& on, at::ScalarType st, std::initializer_list<int64_t> sizes, const char* name, bool may_be_none) {
+    if (o == Py_None && may_be_none) return nullptr;
+    const at::Tensor& t = tensor(o);
+    on.check(t, name);
+    bool ok = t.scalar_type() == st && t.dim() == (int64_t)sizes.size() && t.is_contiguous();
+    int64_t i = 0;
+    for (int64_t s : sizes) { ok = ok && (s < 0 || t.size(i) == s); ++i; }
+    if (!ok) fail(PyExc_ValueError, "%s must be a contiguous %s tensor of the documented shape", name, c10::toString(st));
+    return &t;
+}
+void strides_of(const at::Tensor& t, int64_t* s) { s[0] = t.stride(0); s[1] = t.stride(1); s[2] = t.stride(2); }
+// a [batch, heads, rows, head_dim] tensor with a contiguous last dimension
+const at::Tensor* heads4(PyObject* o, const OnDevice& on, const char* name) {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o);
+    on.check(t, name);
+    if (t.dim() != 4) fail(PyExc_ValueError, "%s must have four dimensions", name);
+    if (t.stride(3) != 1) fail(PyExc_ValueError, "last dimension of %s must be contiguous", name);
+    return &t;
+}
+bool same_shape(const at::Tensor& x, const at::Tensor& y) { return x.sizes() == y.sizes(); }
+
+// (Q | None, K | None, q_weight | None, k_weight | None, inv_freq | None, first, offset | None, shift, eps, interleaved,
+//  q_out | None, k_out | None) -> (status, q_out, k_out)
+PyObject* qk_norm_rope(PyObject* const* a, Py_ssize_t na) {
+    want_args(na, 12);
+    if (a[0] == Py_None && a[1] == Py_None) fail(PyExc_ValueError, "Q or K is needed");
+    const OnDevice on(tensor(a[0] == Py_None ? a[1] : a[0]));
+    const at::Tensor *Q = heads4(a[0], on, "Q"), *K = heads4(a[1], on, "K");
+    const at::Tensor& x = Q ? *Q : *K;
+    if (Q && K && (Q->size(0) != K->size(0) || Q->size(2) != K->size(2) || Q->size(3) != K->size(3) || Q->scalar_type() != K->scalar_type()))
+        fail(PyExc_ValueError, "Q and K must agree in batch, tokens, head_dim and dtype");
+    ot_qk_params p{};
+    p.batch = (int32_t)x.size(0); p.n = (int32_t)x.size(2); p.head_dim = (int32_t)x.size(3);
+    if (p.batch != x.size(0) || p.n != x.size(2)) fail(PyExc_ValueError, "batch and tokens must fit 32 bits");
+    p.q_heads = Q ? (int32_t)Q->size(1) : 0; p.kv_heads = K ? (int32_t)K->size(1) : 0;
+    p.dtype = dtype_code(x);
+    const at::Tensor* inv = array(a[4], on, at::kDouble, {-1}, "inv_freq", true);
+    p.rotary_dim = inv ? (int32_t)(2 * inv->numel()) : 0;
+    p.shift = as_int(a[7]); p.eps = (float)as_double(a[8]); p.interleaved = as_int(a[9]);
+    const at::Tensor* qw = array(a[2], on, x.scalar_type(), {p.head_dim}, "q_weight", true);
+    const at::Tensor* kw = array(a[3], on, x.scalar_type(), {p.head_dim}, "k_weight", true);
+    const at::Tensor* first = array(a[5], on, at::kInt, {p.batch}, "first", false);
+    const at::Tensor* offset = array(a[6], on, at::kInt, {p.batch, p.n}, "offset", true);
+    const at::Tensor *qo = heads4(a[10], on, "q_out"), *ko = heads4(a[11], on, "k_out");
+    at::Tensor own_q, own_k;
+    if (Q && !qo) { own_q = at::empty_like(*Q); qo = &own_q; }
+    if (K && !ko) { own_k = at::empty_like(*K); ko = &own_k; }
+    if (Q && (!same_shape(*Q, *qo) || qo->scalar_type() != Q->scalar_type() || qo->stride(3) != 1)) fail(PyExc_ValueError, "q_out must have Q's shape and dtype");
+    if (K && (!same_shape(*K, *ko) || ko->scalar_type() != K->scalar_type() || ko->stride(3) != 1)) fail(PyExc_ValueError, "k_out must have K's shape and dtype");
+    if (Q) { strides_of(*Q, p.q_strides); strides_of(*qo, p.qo_strides); }
+    if (K) { strides_of(*K, p.k_strides); strides_of(*ko, p.ko_strides); }
+    const void *const pq = ptr(Q), *const pk = ptr(K), *const pqw = ptr(qw), *const pkw = ptr(kw);
+    const double* const pi = (const double*)ptr(inv);
+    const int32_t *const pf = (const int32_t*)ptr(first), *const po = (const int32_t*)ptr(offset);
+    void *const oq = Q ? ptr(qo) : nullptr, *const ok = K ? ptr(ko) : nullptr;
+    void* s = on.stream();
+    const int st = without_gil([&] { return ot_qk_norm_rope(&p, pq, pk, pqw, pkw, pi, pf, po, oq, ok, s); });
+    Ref rq(Q ? wrap(*qo) : (Py_INCREF(Py_None), Py_None)), rk(K ? wrap(*ko) : (Py_INCREF(Py_None), Py_None));
+    return Py_BuildValue("iOO", st, rq.p, rk.p);
+}
+
+// (k, v, k_exp | None, v_exp | None, table) of a PagedCache
+ot_paged_cache paged_cache(PyObject* const* a, const OnDevice& on, int64_t batch) {
+    if (a[0] == Py_None || a[1] == Py_None) fail(PyExc_TypeError, "cache.k and cache.v are needed");
+    const at::Tensor &k = *heads4(a[0], on, "cache.k"), &v = *heads4(a[1], on, "cache.v");
+    if (!same_shape(k, v) || k.scalar_type() != v.scalar_type()) fail(PyExc_ValueError, "cache.k and cache.v must agree in shape and dtype");
+    ot_paged_cache c{};
+    c.num_pages = (int32_t)k.size(0); c.kv_heads = (int32_t)k.size(1); c.page_size = (int32_t)k.size(2); c.head_dim = (int32_t)k.size(3);
+    if (c.num_pages != k.size(0)) fail(PyExc_ValueError, "pages must fit 32 bits");
+    const bool eight = k.scalar_type() == at::kByte || k.scalar_type() == at::kFloat8_e4m3fn;
+    if (!eight && k.scalar_type() != at::kBFloat16) fail(PyExc_TypeError, "pages are bfloat16, or uint8 / float8_e4m3fn");
+    c.dtype = eight ? OT_E4M3 : OT_BF16;
+    strides_of(k, c.k_strides); strides_of(v, c.v_strides);
+    c.k_pages = ptr(k); c.v_pages = ptr(v);
+    if (eight) {
+        c.k_exp = (uint8_t*)ptr(array(a[2], on, at::kByte, {k.size(0), k.size(1)}, "cache.k_exp", false));
+        c.v_exp = (uint8_t*)ptr(array(a[3], on, at::kByte, {k.size(0), k.size(1)}, "cache.v_exp", false));
+    }
+    const at::Tensor* table = array(a[4], on, at::kInt, {batch, -1}, "cache.table", false);
+    c.max_pages = (int32_t)table->size(1);
+    c.page_table = (const int32_t*)ptr(table);
+    return c;
+}
+
+// (K, V, cache x 5, cache_len, count | None, rows | None, count_shift, inv_freq | None, shift, interleaved, new_len | None)
+//  -> (status, new_len)
+PyObject* kv_append_paged(PyObject* const* a, Py_ssize_t na) {
+    want_args(na, 15);
+    const OnDevice on(tensor(a[0]));
+    const at::Tensor &V = tensor(a[1]), &K = *heads4(a[0], on, "K");
+    heads4(a[1], on, "V");
+    if (!same_shape(K, V) || K.scalar_type() != V.scalar_type()) fail(PyExc_ValueError, "K and V must agree in shape and dtype");
+    const ot_paged_cache c = paged_cache(a + 2, on, K.size(0));
+    if (K.size(1) != c.kv_heads || K.size(3) != c.head_dim) fail(PyExc_ValueError, "K and the cache must agree in heads and head_dim");
+    ot_append_params p{};
+    p.batch = (int32_t)K.size(0); p.n = (int32_t)K.size(2);
+    if (p.batch != K.size(0) || p.n != K.size(2)) fail(PyExc_ValueError, "batch and rows must fit 32 bits");
+    p.dtype = dtype_code(K);
+    strides_of(K, p.k_strides); strides_of(V, p.v_strides);
+    const at::Tensor* len = array(a[7], on, at::kInt, {p.batch}, "cache_len", false);
+    const at::Tensor* count = array(a[8], on, at::kInt, {p.batch}, "count", true);
+    const at::Tensor* rows = array(a[9], on, at::kInt, {p.batch, p.n}, "rows", true);
+    p.count_shift = as_int(a[10]);
+    const at::Tensor* inv = array(a[11], on, at::kDouble, {-1}, "inv_freq", true);
+    p.rotary_dim = inv ? (int32_t)(2 * inv->numel()) : 0;
+    p.shift = as_int(a[12]); p.interleaved = as_int(a[13]);
+    at::Tensor own;
+    const at::Tensor* nl = array(a[14], on, at::kInt, {p.batch}, "new_len", true);
+    if (!nl) { own = new_tensor({p.batch}, at::kInt, on.dev); nl = &own; }
+    const void *const pk = ptr(K), *const pv = ptr(V);
+    const double* const pi = (const double*)ptr(inv);
+    const int32_t *const pl = (const int32_t*)ptr(len), *const pc = (const int32_t*)ptr(count), *const pr = (const int32_t*)ptr(rows);
+    int32_t* const po = (int32_t*)ptr(nl);
+    void* s = on.stream();
+    const int st = without_gil([&] { return ot_kv_append_paged(&p, &c, pk, pv, pi, pl, pc, pr, po, s); });
+    Ref o(wrap(*nl));
+    return Py_BuildValue("iO", st, o.p);
+}
+
+// (Q, cache x 5, K_tree | None, V_tree | None, prefix_len, mask | None, out | None, workspace, scale) -> (status, out)
+PyObject* attention_paged(PyObject* const* a, Py_ssize_t na) {
+    want_args(na, 13);
+    const OnDevice on(tensor(a[0]));
+    const at::Tensor& Q = *heads4(a[0], on, "Q");
+    const ot_paged_cache c = paged_cache(a + 1, on, Q.size(0));
+    const at::Tensor *Kt = heads4(a[6], on, "K_tree"), *Vt = heads4(a[7], on, "V_tree");
+    if (Q.scalar_type() != at::kBFloat16 || Q.size(3) != c.head_dim) fail(PyExc_ValueError, "Q must be bfloat16 with the cache's head_dim");
+    if (!Kt != !Vt || (Kt && a[9] == Py_None)) fail(PyExc_ValueError, "K_tree, V_tree and mask come together");
+    if (Kt && (!same_shape(*Kt, *Vt) || Kt->scalar_type() != at::kBFloat16 || Vt->scalar_type() != at::kBFloat16 || Kt->size(0) != Q.size(0) ||
+               Kt->size(1) != c.kv_heads || Kt->size(3) != c.head_dim))
+        fail(PyExc_ValueError, "K_tree and V_tree must be bfloat16 [B, Hkv, keys, D]");
+    ot_paged_attn_params p{};
+    p.batch = (int32_t)Q.size(0); p.q_heads = (int32_t)Q.size(1); p.n = (int32_t)Q.size(2);
+    p.tree_keys = Kt ? (int32_t)Kt->size(2) : 0;
+    p.softmax_scale = (float)as_double(a[12]);
+    const at::Tensor* len = array(a[8], on, at::kInt, {p.batch}, "prefix_len", false);
+    const at::Tensor* mask = Kt ? array(a[9], on, at::kLong, {p.batch, p.n, OT_MASK_WORDS(p.tree_keys)}, "mask", false) : nullptr;
+    at::Tensor own;
+    const at::Tensor* O = heads4(a[10], on, "out");
+    if (!O) { own = at::empty_like(Q); O = &own; }
+    if (!same_shape(Q, *O) || O->scalar_type() != at::kBFloat16 || O->stride(3) != 1) fail(PyExc_ValueError, "out must have Q's shape and dtype");
+    strides_of(Q, p.q_strides); strides_of(*O, p.o_strides);
+    if (Kt) { strides_of(*Kt, p.kt_strides); strides_of(*Vt, p.vt_strides); }
+    const at::Tensor& w = *array(a[11], on, at::kByte, {-1}, "workspace", false);
+    const void *const q = ptr(Q), *const kt = ptr(Kt), *const vt = ptr(Vt);
+    const int32_t* const pl = (const int32_t*)ptr(len);
+    const uint64_t* const pm = (const uint64_t*)ptr(mask);
+    void *const po = ptr(*O), *const pw = ptr(w);
+    const size_t nw = bytes_of(w);
+    void* s = on.stream();
+    const int st = without_gil([&] { return ot_tree_verify_attention_paged(&p, &c, q, kt, vt, pl, pm, po, pw, nw, s); });
+    Ref o(wrap(*O));
+    return Py_BuildValue("iO", st, o.p);
+}
+
 // ---- prepared calls: everything but the stream fixed beforehand; called as f(stream) -> status -----------------------
 struct PreparedBuild {
     ot_build_params p; const void* logits; void* ws; size_t bytes; ot_tree_out out;
@@ -503,7 +676,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
 #define OT_METHOD(name) {#name, (PyCFunction)(void (*)(void))entry<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {OT_METHOD(build_tree), OT_METHOD(build_tree_adaptive), OT_METHOD(stream_begin), OT_METHOD(stream_expand),
                          OT_METHOD(stream_mask), OT_METHOD(stream_esub), OT_METHOD(stream_finalize), OT_METHOD(attention),
-                         OT_METHOD(attention_fp8kv), OT_METHOD(verify), OT_METHOD(kv_append), OT_METHOD(prepare_build),
+                         OT_METHOD(attention_fp8kv), OT_METHOD(verify), OT_METHOD(kv_append), OT_METHOD(qk_norm_rope), OT_METHOD(kv_append_paged),
+                         OT_METHOD(attention_paged), OT_METHOD(prepare_build),
                          OT_METHOD(prepare_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
