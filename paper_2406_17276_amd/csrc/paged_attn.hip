@@ -11,6 +11,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "internal.h"
@@ -27,6 +28,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned long long u64;
 
 constexpr float kLog2e = 1.4426950408889634f;
+// Page numbers are read through the scalar cache (nothing writes the table while a call runs): as vector loads they would
+// queue behind the K and V rows in flight, and waiting for one would wait for all of those.
+typedef const int32_t __attribute__((address_space(4))) * scalar_int;
 constexpr int kCounters = OT_PAGED_SYNC_BYTES / 4 - 1024;   // tickets, behind the kilo-word that ends with the status word
 constexpr int kSplitBatch = 256;                             // sequences of a batch whose contexts are cut into ranges
 constexpr int kTile = 64;
@@ -36,19 +40,27 @@ constexpr float kNoRef = -3.402823466e38f;
 // bf16, and most tiles then rescale nothing.
 constexpr float kSlack = 8.f;
 
+// What the first loads of a workgroup wait for, as leading scalar arguments: the hardware hands these over in registers at
+// wavefront start (kernel-argument preload).
+struct Lead {
+    const int32_t *prefix_len, *table;
+    int batch, units, max_pages, ps_log2, tiles_tree, ranges;      // ranges: jobs aimed at << 8 | fewest tiles of a range; 0: no ranges
+};
+#define OT_LEAD_PARAMS const int32_t *l_prefix_len, const int32_t *l_table, const int l_batch, const int l_units, const int l_max_pages, \
+                       const int l_ps_log2, const int l_tiles_tree, const int l_ranges
+#define OT_LEAD Lead{l_prefix_len, l_table, l_batch, l_units, l_max_pages, l_ps_log2, l_tiles_tree, l_ranges}
+
 struct PagedArgs {
     const void *Q, *Kt, *Vt;
     const unsigned char *kp, *vp;
     const unsigned char *k_exp, *v_exp;
-    const int32_t *table, *prefix_len;
     const uint64_t* mask;
     void* O;
     unsigned int* sync;
     float* part;                 // [job][rows of a block][D], then [job][rows][2] (reference, sum)
     float* part_ml;
-    int batch, kv_heads, g, n, tree_keys, W, row_blocks, units;   // units = kv_heads * row_blocks
-    int num_pages, max_pages, ps_log2;
-    int split, target, least;    // ranges allowed; jobs aimed at; fewest tiles of a range
+    int kv_heads, g, n, tree_keys, W, row_blocks, units;          // units = kv_heads * row_blocks
+    int num_pages;
     int slot_rows;               // rows of a partial
     float scale_log2;
     long long qs[3], kts[3], vts[3], os[3], kps[3], vps[3];
@@ -62,14 +74,13 @@ __device__ __forceinline__ float xhalf_sum(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ int wave_sum_i(int v) {
-    v = wave_incl_scan(v, 0);
-    return rl(v, 63);
-}
+__device__ __forceinline__ int wave_sum_i(int v) { return rl(wave_incl_scan(v, 0), 63); }
 __device__ __forceinline__ int wave_max_i(int v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = max(v, __shfl_xor(v, o));
-    return __builtin_amdgcn_readfirstlane(v);
+    v = max(v, dpp_i<DPP_QUAD_XOR1>(v, v));
+    v = max(v, dpp_i<DPP_QUAD_XOR2>(v, v));
+    v = max(v, dpp_i<DPP_ROW_HALF_MIRROR>(v, v));
+    v = max(v, dpp_i<DPP_ROW_MIRROR>(v, v));
+    return max(max(rl(v, 0), rl(v, 16)), max(rl(v, 32), rl(v, 48)));
 }
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -82,49 +93,55 @@ struct Job {
     bool none;
 };
 
-// Which range of which unit workgroup `wg` computes; the same in every lane of the workgroup.  With more than one range to go
-// round, tiles per range are the fewest (at least a.least) with which all jobs together are no more than a.target: each
-// sequence takes ceil(tiles / share) ranges of equal length.  Lane j holds sequences j, j + 64, ...
-__device__ __forceinline__ Job find_job(const PagedArgs& a, int wg) {
+// Which range of which unit workgroup `wg` computes; the same in every lane of the workgroup.  Tiles per range are about the
+// fewest (at least `least`) with which all jobs together are no more than `target`: each sequence takes ceil(tiles / share)
+// ranges of equal length.  Lane j holds sequences j, j + 64, ...
+__device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int wg) {
     const int lane = threadIdx.x & 63, cap = a.max_pages << a.ps_log2;
-    const int ttiles = (a.tree_keys + kTile - 1) / kTile;
     Job j;
     j.none = false;
-    if (!a.split) {
+    int raw;
+    if (!a.ranges) {
         j.b = wg / a.units;
         j.unit = wg - j.b * a.units;
         j.splits = 1; j.split = 0; j.slot = 0;
         if (j.b >= a.batch) { j.none = true; return j; }
+        raw = a.prefix_len[j.b];
     } else {
         constexpr int NL = kSplitBatch / 64;
-        int T[NL], S[NL], total = 0, most = 0;
+        const int target = a.ranges >> 8, least = a.ranges & 255;
+        const int u = wg / a.units;                      // which (sequence, range)
+        j.unit = wg - u * a.units;
+        int len[NL], T[NL], S[NL], most = 0;
+        float total = 0.f;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
             const int b = lane + 64 * i;
-            T[i] = b < a.batch ? (min(max(a.prefix_len[b], 0), cap) + kTile - 1) / kTile + ttiles : 0;
+            len[i] = b < a.batch ? a.prefix_len[b] : 0;
         }
 #pragma unroll
         for (int i = 0; i < NL; ++i)
-            if (i == 0 || a.batch > 64 * i) { total += wave_sum_i(T[i]); most = max(most, wave_max_i(T[i])); }
-        const long long all = (long long)total * a.units;
-        int share = max(a.least, (int)min((long long)most, (all + a.target - 1) / a.target));
+            if (i == 0 || a.batch > 64 * i) {
+                T[i] = lane + 64 * i < a.batch ? (min(max(len[i], 0), cap) + kTile - 1) / kTile + a.tiles_tree : 0;
+                total += (float)wave_sum_i(T[i]);
+                most = max(most, wave_max_i(T[i]));
+            }
+        int share = max(least, min(most, (int)ceilf(total * (float)a.units / (float)target)));
         int jobs;
         while (true) {
             jobs = 0;
 #pragma unroll
             for (int i = 0; i < NL; ++i)
                 if (i == 0 || a.batch > 64 * i) {
-                    S[i] = lane + 64 * i < a.batch ? max(1, (T[i] + share - 1) / share) : 0;
+                    S[i] = lane + 64 * i < a.batch ? max(1, (int)((unsigned)(T[i] + share - 1) / (unsigned)share)) : 0;
                     jobs += wave_sum_i(S[i]);
                 }
-            if ((long long)jobs * a.units <= a.target || share >= most) break;
+            if (jobs <= target / a.units || share >= most) break;
             share += max(1, share >> 4);
         }
-        const int u = wg / a.units;                      // which (sequence, range)
         if (u >= jobs) { j.none = true; return j; }
-        j.unit = wg - u * a.units;
         int before = 0;
-        j.b = 0; j.split = 0; j.splits = 1;
+        j.b = 0; j.split = 0; j.splits = 1; raw = 0;
 #pragma unroll
         for (int i = 0; i < NL; ++i)
             if (i == 0 || a.batch > 64 * i) {
@@ -135,20 +152,21 @@ __device__ __forceinline__ Job find_job(const PagedArgs& a, int wg) {
                     j.b = 64 * i + l;
                     j.splits = rl(S[i], l);
                     j.split = u - (rl(end, l) - j.splits);
+                    raw = rl(len[i], l);
                 }
                 before = rl(end, 63);
             }
         j.slot = wg - j.split * a.units;                 // of the unit's first range
     }
-    const int raw = a.prefix_len[j.b];
+    raw = uniform(raw);
     j.len = min(max(raw, 0), cap);
     if (j.len != raw && threadIdx.x == 0)
-        __hip_atomic_fetch_or(a.sync + OT_ATTN_STATUS_OFFSET / 4, OT_ATTN_STATUS_PREFIX_CLAMPED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const long long Tb = (j.len + kTile - 1) / kTile + ttiles;
-    j.t0 = (int)(Tb * j.split / j.splits);
-    j.t1 = (int)(Tb * (j.split + 1) / j.splits);
-    j.b = uniform(j.b); j.unit = uniform(j.unit); j.len = uniform(j.len); j.t0 = uniform(j.t0); j.t1 = uniform(j.t1);
-    j.splits = uniform(j.splits); j.split = uniform(j.split); j.slot = uniform(j.slot);
+        __hip_atomic_fetch_or(sync + OT_ATTN_STATUS_OFFSET / 4, OT_ATTN_STATUS_PREFIX_CLAMPED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    j.b = uniform(j.b); j.unit = uniform(j.unit); j.splits = uniform(j.splits); j.split = uniform(j.split); j.slot = uniform(j.slot);
+    // the first ranges take a tile more each where the tiles do not divide
+    const unsigned Tb = (unsigned)((j.len + kTile - 1) / kTile + a.tiles_tree), each = Tb / (unsigned)j.splits, over = Tb - each * (unsigned)j.splits;
+    j.t0 = uniform((int)(each * (unsigned)j.split + min((unsigned)j.split, over)));
+    j.t1 = uniform(j.t0 + (int)(each + ((unsigned)j.split < over ? 1u : 0u)));
     return j;
 }
 
@@ -193,10 +211,11 @@ template <int D> __device__ __forceinline__ int v_swizzle(int r) { return D == 1
 // B operands of the two 16-key slabs, and rescales what the row has summed when the reference moves.
 template <int NO>
 __device__ __forceinline__ void softmax_block(f32x16& s, float c, float& ref, float& l, f32x16 (&o)[NO], u32x4 (&p)[2]) {
-    float m = max3(s[0], s[1], s[2]);
+    // (compiler-made maxima: an assembly one would not wait for the matrix instruction that makes its operand)
+    float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
-    for (int v = 3; v < 15; v += 2) m = max3(m, s[v], s[v + 1]);
-    m = xhalf_max(max2(m, s[15])) * c;
+    for (int v = 3; v < 15; v += 2) m = fmaxf(fmaxf(m, s[v]), s[v + 1]);
+    m = xhalf_max(fmaxf(m, s[15])) * c;
     if (__any(m > ref + kSlack)) {
         const float to = m > ref + kSlack ? m : ref, f = __builtin_amdgcn_exp2f(ref - to);
         l *= f;
@@ -245,120 +264,147 @@ __device__ __forceinline__ unsigned short* out_row(const PagedArgs& a, int b, in
 
 // After a workgroup has stored its partial: the last one of its row block adds all of them up, in the order of the ranges.
 template <int D, int NT>
-__device__ __forceinline__ void join_splits(const PagedArgs& a, const Job& j, int hk, int row0, int rows) {
-    __shared__ int s_last;
+__device__ __forceinline__ void join_splits(const PagedArgs& a, const Job& j, int hk, int row0, int rows, int* s_last) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     unsigned int* const ticket = a.sync + 1024 + j.b * a.units + j.unit;
     if (threadIdx.x == 0)
-        s_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(j.splits - 1);
+        *s_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(j.splits - 1);
     __syncthreads();
-    if (!s_last) return;
+    if (!*s_last) return;
     if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = threadIdx.x; i < rows * (D / 8); i += NT) {
-        const int row = i / (D / 8), col = i % (D / 8) * 8;
-        float M = kNoRef, L = 0.f, o[8];
+    // a thread adds up two columns of a row (few rows: every thread has some) or eight; all loads of a chunk of ranges are
+    // requested before the first is used, each is a trip to memory
+    auto join = [&](auto words_c, auto chunk_c) {
+        constexpr int WORDS = words_c, CHUNK = chunk_c, PER = D / (2 * WORDS);
+        for (int i = threadIdx.x; i < rows * PER; i += NT) {
+            const int row = i / PER, col = i % PER * 2 * WORDS;
+            float M = kNoRef, L = 0.f, o[2 * WORDS];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = 0.f;
-        for (int s = 0; s < j.splits; ++s) {
-            const size_t at = (size_t)(j.slot + s * a.units) * a.slot_rows + row;
-            const float2 ml = get2(a.part_ml + at * 2);
-            const float to = fmaxf(M, ml.x), f = __builtin_amdgcn_exp2f(M - to), w = __builtin_amdgcn_exp2f(ml.x - to);
-            L = L * f + ml.y * w;
+            for (int e = 0; e < 2 * WORDS; ++e) o[e] = 0.f;
+            for (int s0 = 0; s0 < j.splits; s0 += CHUNK) {
+                float2 ml[CHUNK], x[CHUNK][WORDS];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 x = get2(a.part + at * D + col + 2 * e);
-                o[2 * e] = o[2 * e] * f + x.x * w;
-                o[2 * e + 1] = o[2 * e + 1] * f + x.y * w;
+                for (int s = 0; s < CHUNK; ++s) {
+                    const size_t at = (size_t)(j.slot + min(s0 + s, j.splits - 1) * a.units) * a.slot_rows + row;
+                    ml[s] = get2(a.part_ml + at * 2);
+#pragma unroll
+                    for (int e = 0; e < WORDS; ++e) x[s][e] = get2(a.part + at * D + col + 2 * e);
+                }
+                float to = M;
+#pragma unroll
+                for (int s = 0; s < CHUNK; ++s) to = fmaxf(to, ml[s].x);            // (a copy of the last range changes nothing)
+                const float f = __builtin_amdgcn_exp2f(M - to);
+                L *= f;
+#pragma unroll
+                for (int e = 0; e < 2 * WORDS; ++e) o[e] *= f;
+#pragma unroll
+                for (int s = 0; s < CHUNK; ++s) {
+                    const float w = s0 + s < j.splits ? __builtin_amdgcn_exp2f(ml[s].x - to) : 0.f;
+                    L += ml[s].y * w;
+#pragma unroll
+                    for (int e = 0; e < WORDS; ++e) { o[2 * e] += x[s][e].x * w; o[2 * e + 1] += x[s][e].y * w; }
+                }
+                M = to;
             }
-            M = to;
-        }
-        const float inv = inverse(L);
+            const float inv = inverse(L);
+            unsigned short* const to = out_row(a, j.b, hk, row0 + row) + col;
+            if constexpr (WORDS == 1) *(unsigned*)to = pack_bf16(o[0] * inv, o[1] * inv);
+            else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= inv;
-        store8<OT_BF16>(out_row(a, j.b, hk, row0 + row), col, o);
-    }
+                for (int e = 0; e < 2 * WORDS; ++e) o[e] *= inv;
+                store8<OT_BF16>(to, 0, o);
+            }
+        }
+    };
+    if (rows * (D / 2) <= NT) join(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
+    else join(std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
 }
 
 // ---------------------------------------------------------------------------
-// Few rows: 32 or 64 packed query rows per workgroup (QB blocks of 32).
-// Bound by the cache's bytes.  Four wavefronts share a job's keys, 32 at a time, and never wait for each other inside the
-// loop: a wavefront loads its 32 rows of K straight into the registers that feed the matrix instruction (S^T = K Q^T, the
-// order of the contraction is free, so a lane's sixteen consecutive values serve two instructions), and its 32 rows of V into
-// a corner of LDS of its own, from which the transposing read makes the operand of O^T += V^T P^T.  The next block's rows are
-// requested before the present one is used.  Pages are multiples of sixteen rows, so a block's page numbers and exponents are
-// two scalars each.  The four partial results meet in LDS at the end.
+// Few rows: 32 packed query rows per wavefront, QW blocks of them per workgroup (1 or 2).
+// Bound by the cache's bytes.  The four wavefronts are QW row blocks x KS streams of 32-key blocks and never wait for each
+// other inside the loop: a wavefront loads its 32 rows of K straight into the registers that feed the matrix instruction
+// (S^T = K Q^T; the order of the contraction is free, so a lane's sixteen consecutive values serve two instructions), and its 32
+// rows of V into a corner of LDS of its own, from which the transposing read makes the operand of O^T += V^T P^T.  The next
+// block's V is requested as soon as this one's is in LDS, its K as soon as this one's scores are made.  Pages are multiples
+// of sixteen rows, so a block's page numbers and exponents are two scalars each, known a block earlier.  The streams'
+// results meet in LDS at the end.
 // ---------------------------------------------------------------------------
-template <int D, bool KV8, int QB>
-__global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
+template <int D, bool KV8, int QW>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_rows_kernel(OT_LEAD_PARAMS, const PagedArgs a) {
+    constexpr int KS = 4 / QW;
     constexpr int DB = D / 32, NJ = D / 32;
+    constexpr int ESZ = KV8 ? 1 : 2;
     constexpr int KL = KV8 ? NJ : 2 * NJ;              // 16-byte loads of K per lane and block; the same of V
-    constexpr int CPR = (KV8 ? D : 2 * D) / 16;        // 16-byte pieces per row of V in memory
+    constexpr int CPR = D * ESZ / 16;                  // 16-byte pieces per row of V in memory
     constexpr int RPL = 64 / CPR;                      // rows of V per load instruction
     constexpr int VW = 32 * D;                         // a wavefront's V in LDS, 2-byte elements
+    constexpr int KW = 32 * D * ESZ / 2;               // its K, as stored
     constexpr int OST = 68;                            // row stride of the exchange at the end
-    constexpr int kShared = 4 * VW * 2 > 4 * 32 * OST * 4 ? 4 * VW * 2 : 4 * 32 * OST * 4;
-    __shared__ __attribute__((aligned(16))) unsigned char s_mem[kShared];
-    __shared__ float s_ref[4][QB * 32], s_sum[4][QB * 32];
-    __shared__ u64 s_union[OT_MAX_TREE_KEYS / 64];
-    const Job j = find_job(a, blockIdx.x);
+    constexpr int kLoop = 4 * (VW + KW) * 2, kEnd = 4 * 32 * OST * 4;
+    // V and K of the four wavefronts, then Q.  The union of the masks takes the place of K once the cache is through, the
+    // exchange that of V and K, its scalars that of Q: 80 KB at most, so that two workgroups share a compute unit.
+    constexpr int kMem = kLoop > kEnd ? kLoop : kEnd;
+    __shared__ __attribute__((aligned(16))) unsigned char s_mem[kMem + QW * 32 * D * 2];
+    static_assert(sizeof(s_mem) <= 80 * 1024 && 4 * KW * 2 >= OT_MAX_TREE_KEYS / 8 && QW * 32 * D * 2 >= 4 * 32 * 8 + 4, "LDS");
+    u64* const s_union = (u64*)(s_mem + 4 * VW * 2);
+    float* const s_ref = (float*)(s_mem + kMem);                             // [4][32]
+    float* const s_sum = s_ref + 4 * 32;
+    int* const s_last = (int*)(s_sum + 4 * 32);
+    const Job j = find_job(OT_LEAD, a.sync, blockIdx.x);
     if (j.none) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, h = lane >> 5;
+    const int qb = wave % QW, ks = wave / QW;
     const int hk = j.unit / a.row_blocks, rb = j.unit - hk * a.row_blocks;
-    const int rows_all = a.g * a.n, row0 = rb * QB * 32, rows = min(QB * 32, rows_all - row0);
+    const int rows_all = a.g * a.n, row0 = rb * QW * 32, rows = min(QW * 32, rows_all - row0);
 
-    // Q: lane (query l32, half h) holds columns 32 i + 16 h .. + 15
-    bf16x8 qf[QB][2 * NJ];
-    long long mask_at[QB];
+    // Q in LDS, one copy per row block: lane (query l32, half h) reads columns 32 i + 16 h .. + 15, 16-byte piece p of query r at
+    // p ^ (r mod D/8)
+    unsigned short* const s_q = (unsigned short*)(s_mem + kMem);
+    long long mask_at;
+    {
+        const int rho = min(row0 + qb * 32 + l32, rows_all - 1), head = rho / a.n, node = rho - head * a.n;
+        mask_at = ((long long)j.b * a.n + node) * a.W;
+        if (ks == 0) {
+            const unsigned short* p = (const unsigned short*)a.Q + (long long)j.b * a.qs[0] + (long long)(hk * a.g + head) * a.qs[1] +
+                                      (long long)node * a.qs[2];
 #pragma unroll
-    for (int q = 0; q < QB; ++q) {
-        const int rho = min(row0 + q * 32 + l32, rows_all - 1), head = rho / a.n, node = rho - head * a.n;
-        const unsigned short* p = (const unsigned short*)a.Q + (long long)j.b * a.qs[0] + (long long)(hk * a.g + head) * a.qs[1] +
-                                  (long long)node * a.qs[2] + 16 * h;
-        mask_at[q] = ((long long)j.b * a.n + node) * a.W;
-#pragma unroll
-        for (int i = 0; i < NJ; ++i) {
-            qf[q][2 * i] = __builtin_bit_cast(bf16x8, *(const u32x4*)(p + 32 * i));
-            qf[q][2 * i + 1] = __builtin_bit_cast(bf16x8, *(const u32x4*)(p + 32 * i + 8));
+            for (int i = 0; i < D / 16; ++i) {
+                const int at = 2 * i + h;
+                *(u32x4*)(s_q + (qb * 32 + l32) * D + ((at ^ (l32 & (D / 8 - 1))) << 3)) = *(const u32x4*)(p + 8 * at);
+            }
         }
     }
+    __syncthreads();
+    const unsigned short* const q_row = s_q + (qb * 32 + l32) * D;
+    auto q_frag = [&](int i) {                           // piece 4 (i / 2) + 2 h + i % 2
+        return __builtin_bit_cast(bf16x8, *(const u32x4*)(q_row + (((4 * (i >> 1) + 2 * h + (i & 1)) ^ (l32 & (D / 8 - 1))) << 3)));
+    };
     const float c = a.scale_log2;
-    float ref[QB], l[QB];
-    f32x16 o[QB][DB];
+    float ref = kNoRef, l = 0.f;
+    f32x16 o[DB];
 #pragma unroll
-    for (int q = 0; q < QB; ++q) {
-        ref[q] = kNoRef; l[q] = 0.f;
+    for (int d = 0; d < DB; ++d)
 #pragma unroll
-        for (int d = 0; d < DB; ++d)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) o[q][d][v] = 0.f;
-    }
+        for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
 
     unsigned short* const s_v = (unsigned short*)s_mem + wave * VW;
+    // K rows in LDS: 16-byte piece c of row r at c ^ (the row's number among those that share a 256-byte line's place)
+    unsigned short* const s_k = (unsigned short*)s_mem + 4 * VW + wave * KW;
+    auto k_at = [](int row, int piece) { return row * (CPR * 8) + ((piece ^ ((row / (16 / CPR)) & (CPR - 1))) << 3); };
     const int tr_j = (lane & 15) >> 2, vx = ((lane >> 4) & 1) ^ v_swizzle<D>(tr_j);
     const unsigned short* const v_read = s_v + (4 * h + tr_j) * D + 4 * (lane & 3);
-
-    // the products of a block: kf(i) the A operands of its keys, V in s_v
-    auto block = [&](const bf16x8 (&kf)[2 * NJ], auto bits_of, bool all) {
-        u32x4 p[QB][2];
-#pragma unroll
-        for (int q = 0; q < QB; ++q) {
-            f32x16 s;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[v] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 2 * NJ; ++i) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf[q][i], s, 0, 0, 0);
-            if (!all) hide(s, bits_of(q), h);
-            softmax_block<DB>(s, c, ref[q], l[q], o[q], p[q]);
-        }
+    // probabilities of a block's scores, times V in s_v
+    auto finish = [&](f32x16& s) {
+        u32x4 p[2];
+        softmax_block<DB>(s, c, ref, l, o, p);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int d = 0; d < DB; ++d) {
                 const bf16x8 vf = column_of_8_rows(v_read + 16 * u * D + (((2 * d) ^ vx) << 4), 8 * D);
-#pragma unroll
-                for (int q = 0; q < QB; ++q)
-                    o[q][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[q][u]), o[q][d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[u]), o[d], 0, 0, 0);
             }
     };
     auto wave_fence = [] {
@@ -368,67 +414,69 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
 
     // ---- cache ----
     const int blocks = (j.len + 31) / 32, ptiles = (j.len + kTile - 1) / kTile;
-    struct Raw {
-        u32x4 k[KL], v[KL];
-        int ke[2], ve[2];
-        unsigned seen;
-    };
-    const int32_t* const table = a.table + (long long)j.b * a.max_pages;
-    const int ps = 1 << a.ps_log2, page_last = max(j.len - 1, 0) >> a.ps_log2;
-    constexpr int ESZ = KV8 ? 1 : 2;
-    const unsigned k_lane = (unsigned)(l32 & 15) * (unsigned)(a.kps[2] * ESZ) + 16 * h * ESZ;
+    const scalar_int table = (scalar_int)l_table + (long long)j.b * l_max_pages;
+    const int ps = 1 << l_ps_log2, page_last = max(j.len - 1, 0) >> l_ps_log2;
     bool bad = false;
-    auto load = [&](int i, Raw& r) {                     // block i: cache rows 32 i .. 32 i + 31
+    struct Pages {
+        int page[2];               // of the block's first and second sixteen rows
+        unsigned seen;             // its rows that exist
+    };
+    auto pages_of = [&](int i) {
+        Pages r;
         const int key0 = 32 * i, rem = j.len - key0;
-        r.seen = rem >= 32 ? 0xffffffffu : (1u << rem) - 1;
-        const unsigned char *kb[2], *vb[2];
+        r.seen = rem >= 32 ? 0xffffffffu : rem > 0 ? (1u << rem) - 1 : 0;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            int page = table[min((key0 + 16 * e) >> a.ps_log2, page_last)];
-            if ((unsigned)page >= (unsigned)a.num_pages) {
-                if (key0 + 16 * e < j.len) bad = true;
-                page = 0;
+        for (int e = 0; e < 2; ++e) r.page[e] = table[min((key0 + 16 * e) >> l_ps_log2, page_last)];
+        return r;
+    };
+    auto check = [&](int i, Pages& r) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if ((unsigned)r.page[e] >= (unsigned)a.num_pages) {
+                if (32 * i + 16 * e < j.len) bad = true;
+                r.page[e] = 0;
                 r.seen &= e ? 0xffffu : 0xffff0000u;
             }
-            const int row = (key0 + 16 * e) & (ps - 1);
-            kb[e] = a.kp + ((long long)page * a.kps[0] + (long long)hk * a.kps[1] + (long long)row * a.kps[2]) * ESZ;
-            vb[e] = a.vp + ((long long)page * a.vps[0] + (long long)hk * a.vps[1] + (long long)row * a.vps[2]) * ESZ;
-            if constexpr (KV8) {
-                r.ke[e] = a.k_exp[(long long)page * a.kv_heads + hk];
-                r.ve[e] = a.v_exp[(long long)page * a.kv_heads + hk];
-            }
-        }
-        const unsigned char* const km = (l32 & 16 ? kb[1] : kb[0]) + k_lane;
-#pragma unroll
-        for (int n = 0; n < KL; ++n) r.k[n] = *(const u32x4*)(km + (KV8 ? 32 * n : 64 * (n >> 1) + 16 * (n & 1)));
-#pragma unroll
-        for (int n = 0; n < KL; ++n) {
-            const int row = n * RPL, e = row >> 4;       // rows row .. row + RPL - 1 of the block
-            r.v[n] = *(const u32x4*)(vb[e] + (unsigned)((row & 15) + lane / CPR) * (unsigned)(a.vps[2] * ESZ) + 16 * (lane % CPR));
-        }
     };
-    auto use = [&](Raw& r) {
-        bf16x8 kf[2 * NJ];
-        if constexpr (KV8) {
-            const float ks = exp_scale(l32 & 16 ? r.ke[1] : r.ke[0]);
+    constexpr int DIST = 1;         // blocks requested ahead
+    u32x4 kr[DIST][KL], vr[DIST][KL];
+    int ke[DIST], ve[DIST][2];                           // exponents: of this lane's key, of either half of the block
+    // Every instruction asks for whole rows, and says that they are read once: 16 bytes of 32 rows each instead, as the matrix
+    // operand wants them, or without the hint, 64 heads over 4 x 100000 keys take 172 us, not 156.
+    const unsigned k_lane = (unsigned)(lane / CPR) * (unsigned)(a.kps[2] * ESZ) + 16 * (lane % CPR);
+    const unsigned v_lane = (unsigned)(lane / CPR) * (unsigned)(a.vps[2] * ESZ) + 16 * (lane % CPR);
+    const unsigned char* const kh = a.kp + (long long)hk * a.kps[1] * ESZ;
+    const unsigned char* const vh = a.vp + (long long)hk * a.vps[1] * ESZ;
+    auto load_k = [&](int i, const Pages& r, int at) {
+        const unsigned char* b[2];
 #pragma unroll
-            for (int i = 0; i < NJ; ++i) {
-                u32x4 lo, hi;
-                widen16(r.k[i], ks, lo, hi);
-                kf[2 * i] = __builtin_bit_cast(bf16x8, lo);
-                kf[2 * i + 1] = __builtin_bit_cast(bf16x8, hi);
-            }
-        } else {
+        for (int e = 0; e < 2; ++e) b[e] = kh + ((long long)r.page[e] * a.kps[0] + (long long)((32 * i + 16 * e) & (ps - 1)) * a.kps[2]) * ESZ;
+        if constexpr (KV8) ke[at] = a.k_exp[(long long)(l32 & 16 ? r.page[1] : r.page[0]) * a.kv_heads + hk];
 #pragma unroll
-            for (int i = 0; i < 2 * NJ; ++i) kf[i] = __builtin_bit_cast(bf16x8, r.k[i]);
+        for (int n = 0; n < KL; ++n)                     // rows n RPL .. n RPL + RPL - 1 of the block
+            kr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + (long long)((n * RPL) & 15) * a.kps[2] * ESZ + k_lane));
+    };
+    auto load_v = [&](int i, const Pages& r, int at) {
+        const unsigned char* b[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            b[e] = vh + ((long long)r.page[e] * a.vps[0] + (long long)((32 * i + 16 * e) & (ps - 1)) * a.vps[2]) * ESZ;
+            if constexpr (KV8) ve[at][e] = a.v_exp[(long long)r.page[e] * a.kv_heads + hk];
         }
-        const float vs[2] = {KV8 ? exp_scale(r.ve[0]) : 1.f, KV8 ? exp_scale(r.ve[1]) : 1.f};
+#pragma unroll
+        for (int n = 0; n < KL; ++n)
+            vr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + (long long)((n * RPL) & 15) * a.vps[2] * ESZ + v_lane));
+    };
+    auto stage = [&](unsigned seen, int slot) {
         wave_fence();
+#pragma unroll
+        for (int n = 0; n < KL; ++n) *(u32x4*)(s_k + k_at(n * RPL + lane / CPR, lane % CPR)) = kr[slot][n];
+        const float vs[2] = {KV8 ? exp_scale(ve[slot][0]) : 1.f, KV8 ? exp_scale(ve[slot][1]) : 1.f};
 #pragma unroll
         for (int n = 0; n < KL; ++n) {
             const int row = n * RPL + lane / CPR, at = lane % CPR;
-            u32x4 w = r.v[n];
-            if (r.seen != 0xffffffffu && !(r.seen >> row & 1)) w = u32x4{0, 0, 0, 0};
+            u32x4 w = vr[slot][n];
+            if (seen != 0xffffffffu && !(seen >> row & 1)) w = u32x4{0, 0, 0, 0};
             if constexpr (KV8) {
                 u32x4 lo, hi;
                 widen16(w, vs[(n * RPL) >> 4], lo, hi);
@@ -439,22 +487,65 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
             }
         }
         wave_fence();
-        const unsigned seen = r.seen;
-        block(kf, [&](int) { return seen; }, seen == 0xffffffffu);
+    };
+    auto scores = [&](int e) {                           // e: exponent of this lane's key
+        f32x16 s;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[v] = 0.f;
+        const float f = KV8 ? exp_scale(e) : 1.f;
+#pragma unroll
+        for (int i = 0; i < NJ; ++i) {
+            u32x4 lo, hi;
+            if constexpr (KV8) widen16(*(const u32x4*)(s_k + k_at(l32, 2 * i + h)), f, lo, hi);
+            else {
+                lo = *(const u32x4*)(s_k + k_at(l32, 4 * i + 2 * h));
+                hi = *(const u32x4*)(s_k + k_at(l32, 4 * i + 2 * h + 1));
+            }
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), q_frag(2 * i), s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), q_frag(2 * i + 1), s, 0, 0, 0);
+        }
+        return s;
     };
     {
         const int end = min(2 * j.t1, blocks);
-        int i = 2 * j.t0 + wave;
-        Raw r0, r1;
-        if (i < end) load(i, r0);
-        while (i < end) {
-            if (i + 4 < end) load(i + 4, r1);
-            use(r0);
-            i += 4;
-            if (i >= end) break;
-            if (i + 4 < end) load(i + 4, r0);
-            use(r1);
-            i += 4;
+        int i = 2 * j.t0 + ks;
+        if (i < end) {
+            // Requests past the last block read that one again: a load under a condition would make every wait for an older one
+            // a wait for all.
+            auto in_range = [&](int k) { return min(k, end - 1); };
+            unsigned seen[DIST];
+#pragma unroll
+            for (int d = 0; d < DIST; ++d) {
+                const int k = in_range(i + d * KS);
+                Pages p = pages_of(k);
+                check(k, p);
+                load_v(k, p, d);
+                load_k(k, p, d);
+                seen[d] = p.seen;
+            }
+            Pages ahead = pages_of(in_range(i + DIST * KS));
+            // block i is in slot `slot`; true: there is another one
+            auto step = [&](auto slot_c) {
+                constexpr int slot = slot_c;
+                const int to = in_range(i + DIST * KS);
+                const Pages after = pages_of(in_range(i + DIST * KS + KS));
+                check(to, ahead);
+                const unsigned now = seen[slot];
+                const int e = KV8 ? ke[slot] : 0;
+                stage(now, slot);
+                __builtin_amdgcn_sched_barrier(0);
+                load_v(to, ahead, slot);
+                load_k(to, ahead, slot);
+                __builtin_amdgcn_sched_barrier(0);
+                f32x16 s = scores(e);
+                if (now != 0xffffffffu) hide(s, now, h);
+                finish(s);
+                seen[slot] = ahead.seen;
+                ahead = after;
+                i += KS;
+                return i < end;
+            };
+            while (step(std::integral_constant<int, 0>()) && (DIST == 1 || step(std::integral_constant<int, DIST - 1>()))) {}
         }
     }
     if (bad && lane == 0)
@@ -463,18 +554,19 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
     // ---- tree ----
     const int tt0 = max(j.t0 - ptiles, 0), tt1 = j.t1 - ptiles;
     if (tt1 > tt0) {
+        __syncthreads();                                 // no wavefront reads K from LDS any more
         union_masks(a, j.b, tt0, tt1, s_union, 256);
         const unsigned short* const kt = (const unsigned short*)a.Kt + (long long)j.b * a.kts[0] + (long long)hk * a.kts[1];
         const unsigned short* const vt = (const unsigned short*)a.Vt + (long long)j.b * a.vts[0] + (long long)hk * a.vts[1];
-        for (int i = 2 * tt0 + wave; i < 2 * tt1 && 32 * i < a.tree_keys; i += 4) {
+        for (int i = 2 * tt0 + ks; i < 2 * tt1 && 32 * i < a.tree_keys; i += KS) {
             const int last = a.tree_keys - 1;
             const unsigned any = (unsigned)(s_union[(i >> 1) - tt0] >> (32 * (i & 1)));
-            const unsigned short* const kr = kt + (long long)min(32 * i + l32, last) * a.kts[2] + 16 * h;
-            bf16x8 kf[2 * NJ];
+            const unsigned short* const k1 = kt + (long long)min(32 * i + l32, last) * a.kts[2] + 16 * h;
+            u32x4 k[2 * NJ];
 #pragma unroll
             for (int n = 0; n < NJ; ++n) {
-                kf[2 * n] = __builtin_bit_cast(bf16x8, *(const u32x4*)(kr + 32 * n));
-                kf[2 * n + 1] = __builtin_bit_cast(bf16x8, *(const u32x4*)(kr + 32 * n + 8));
+                k[2 * n] = *(const u32x4*)(k1 + 32 * n);
+                k[2 * n + 1] = *(const u32x4*)(k1 + 32 * n + 8);
             }
             constexpr int P = D / 8, R = 64 / P;
             wave_fence();
@@ -486,54 +578,66 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
                 *(u32x4*)(s_v + row * D + (((at >> 1) ^ v_swizzle<D>(row)) << 4) + 8 * (at & 1)) = w;
             }
             wave_fence();
+            f32x16 s;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) s[v] = 0.f;
+#pragma unroll
+            for (int n = 0; n < 2 * NJ; ++n) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[n]), q_frag(n), s, 0, 0, 0);
             const unsigned tail = 32 * i + 32 <= a.tree_keys ? 0xffffffffu : (1u << (a.tree_keys - 32 * i)) - 1;
-            block(kf, [&](int q) { return (unsigned)(a.mask[mask_at[q] + (i >> 1)] >> (32 * (i & 1))) & tail; }, false);
+            hide(s, (unsigned)(a.mask[mask_at + (i >> 1)] >> (32 * (i & 1))) & tail, h);
+            finish(s);
         }
     }
 
-    // ---- the four wavefronts' results ----
-#pragma unroll
-    for (int q = 0; q < QB; ++q) {
-        const float sum = xhalf_sum(l[q]);
-        if (h == 0) { s_ref[wave][q * 32 + l32] = ref[q]; s_sum[wave][q * 32 + l32] = sum; }
+    // ---- the streams' results ----
+    __syncthreads();                                     // no wavefront reads Q any more
+    {
+        const float sum = xhalf_sum(l);
+        if (h == 0) { s_ref[wave * 32 + l32] = ref; s_sum[wave * 32 + l32] = sum; }
     }
     __syncthreads();
     float* const s_o = (float*)s_mem;
     const int row = tid >> 3, col = (tid & 7) * 8;
+    float M4 = kNoRef;
 #pragma unroll
-    for (int q = 0; q < QB; ++q) {
-        const float M4 = fmaxf(fmaxf(s_ref[0][q * 32 + l32], s_ref[1][q * 32 + l32]), fmaxf(s_ref[2][q * 32 + l32], s_ref[3][q * 32 + l32]));
-        const float f = __builtin_amdgcn_exp2f(ref[q] - M4);
-        float M = kNoRef, L = 0.f;
+    for (int w = 0; w < KS; ++w) M4 = fmaxf(M4, s_ref[(w * QW + qb) * 32 + l32]);
+    const float f = __builtin_amdgcn_exp2f(ref - M4);
+    float M[QW], L[QW];
 #pragma unroll
-        for (int w = 0; w < 4; ++w) M = fmaxf(M, s_ref[w][q * 32 + row]);
+    for (int q = 0; q < QW; ++q) {
+        M[q] = kNoRef; L[q] = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) L += s_sum[w][q * 32 + row] * __builtin_amdgcn_exp2f(s_ref[w][q * 32 + row] - M);
-        const bool live = q * 32 + row < rows;
+        for (int w = 0; w < KS; ++w) M[q] = fmaxf(M[q], s_ref[(w * QW + q) * 32 + row]);
 #pragma unroll
-        for (int part = 0; part < D / 64; ++part) {
-            __syncthreads();
+        for (int w = 0; w < KS; ++w) L[q] += s_sum[(w * QW + q) * 32 + row] * __builtin_amdgcn_exp2f(s_ref[(w * QW + q) * 32 + row] - M[q]);
+    }
 #pragma unroll
-            for (int d = 0; d < 2; ++d)
+    for (int part = 0; part < D / 64; ++part) {
+        __syncthreads();
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const f32x16& x = o[q][2 * part + d];
-                    *(f32x4*)(s_o + (wave * 32 + l32) * OST + 32 * d + 8 * v + 4 * h) =
-                        f32x4{x[4 * v] * f, x[4 * v + 1] * f, x[4 * v + 2] * f, x[4 * v + 3] * f};
-                }
-            __syncthreads();
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const f32x16& x = o[2 * part + d];
+                *(f32x4*)(s_o + (wave * 32 + l32) * OST + 32 * d + 8 * v + 4 * h) =
+                    f32x4{x[4 * v] * f, x[4 * v + 1] * f, x[4 * v + 2] * f, x[4 * v + 3] * f};
+            }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < QW; ++q) {
+            if (q * 32 + row >= rows) continue;
             float y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const f32x4 lo = *(const f32x4*)(s_o + (w * 32 + row) * OST + col), hi = *(const f32x4*)(s_o + (w * 32 + row) * OST + col + 4);
+            for (int w = 0; w < KS; ++w) {
+                const float* const x = s_o + ((w * QW + q) * 32 + row) * OST + col;
+                const f32x4 lo = *(const f32x4*)x, hi = *(const f32x4*)(x + 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) { y[e] += lo[e]; y[4 + e] += hi[e]; }
             }
-            if (!live) continue;
             if (j.splits == 1) {
-                const float inv = inverse(L);
+                const float inv = inverse(L[q]);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] *= inv;
                 store8<OT_BF16>(out_row(a, j.b, hk, row0 + q * 32 + row), 64 * part + col, y);
@@ -541,11 +645,11 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
                 const size_t at = (size_t)(j.slot + j.split * a.units) * a.slot_rows + q * 32 + row;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) put2(a.part + at * D + 64 * part + col + 2 * e, y[2 * e], y[2 * e + 1]);
-                if (part == 0 && col == 0) put2(a.part_ml + at * 2, M, L);
+                if (part == 0 && col == 0) put2(a.part_ml + at * 2, M[q], L[q]);
             }
         }
     }
-    if (j.splits > 1) join_splits<D, 256>(a, j, hk, row0, rows);
+    if (j.splits > 1) join_splits<D, 256>(a, j, hk, row0, rows, s_last);
 }
 
 // ---------------------------------------------------------------------------
@@ -555,7 +659,7 @@ __global__ __launch_bounds__(256) void paged_rows_kernel(const PagedArgs a) {
 //   K [64][D]: 16-byte piece c of row r at c ^ (r mod D/8);  V [64][D]: 32-byte segment g of row r at g ^ v_swizzle(r)
 // ---------------------------------------------------------------------------
 template <int D, bool KV8, int NW>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tiles_kernel(const PagedArgs a) {
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tiles_kernel(OT_LEAD_PARAMS, const PagedArgs a) {
     constexpr int NT = 64 * NW, DB = D / 32, SL = D / 16, CPR = D / 8;
     constexpr int ESZ = KV8 ? 1 : 2;
     constexpr int CPM = D * ESZ / 16;                  // 16-byte pieces per row in memory
@@ -565,7 +669,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     extern __shared__ __attribute__((aligned(16))) unsigned short s_kv[];       // [2][K, V][64][D]
     __shared__ u64 s_union[OT_MAX_TREE_KEYS / 64];
     constexpr int BUF = 2 * kTile * D;
-    const Job j = find_job(a, blockIdx.x);
+    const Job j = find_job(OT_LEAD, a.sync, blockIdx.x);
     if (j.none) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const int hk = j.unit / a.row_blocks, rb = j.unit - hk * a.row_blocks;
@@ -591,8 +695,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int tr_j = (lane & 15) >> 2, vx = ((lane >> 4) & 1) ^ v_swizzle<D>(tr_j), kx = l32 & (CPR - 1);
 
     const int ptiles = (j.len + kTile - 1) / kTile;
-    const int32_t* const table = a.table + (long long)j.b * a.max_pages;
-    const int ps = 1 << a.ps_log2, page_last = max(j.len - 1, 0) >> a.ps_log2;
+    const scalar_int table = (scalar_int)l_table + (long long)j.b * l_max_pages;
+    const int ps = 1 << l_ps_log2, page_last = max(j.len - 1, 0) >> l_ps_log2;
     const int tt0 = max(j.t0 - ptiles, 0), tt1 = j.t1 - ptiles;
     if (tt1 > tt0) union_masks(a, j.b, tt0, tt1, s_union, NT);
     bool bad = false;
@@ -608,9 +712,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         if (t < ptiles) {
             const int key0 = t * kTile, rem = j.len - key0;
             r.seen = rem >= kTile ? ~0ull : (1ull << rem) - 1;
-            for (int i = 0; i < kTile >> min(a.ps_log2, 6); ++i) {          // pages of the tile that are none
-                const int k0 = key0 + (i << min(a.ps_log2, 6));
-                if (k0 < j.len && (unsigned)table[k0 >> a.ps_log2] >= (unsigned)a.num_pages) {
+            for (int i = 0; i < kTile >> min(l_ps_log2, 6); ++i) {          // pages of the tile that are none
+                const int k0 = key0 + (i << min(l_ps_log2, 6));
+                if (k0 < j.len && (unsigned)table[k0 >> l_ps_log2] >= (unsigned)a.num_pages) {
                     bad = true;
                     const u64 rows_of = ps >= 64 ? ~0ull : ((1ull << (ps & 63)) - 1) << (k0 - key0);
                     r.seen &= ~rows_of;
@@ -619,7 +723,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
             for (int n = 0; n < CH; ++n) {
                 const int first = uniform(wave * (64 / CPM)) + n * (NT / CPM);                    // of the wavefront's rows
-                int page = table[min((key0 + first) >> a.ps_log2, page_last)];
+                int page = table[min((key0 + first) >> l_ps_log2, page_last)];
                 page = (unsigned)page < (unsigned)a.num_pages ? page : 0;
                 const int row = (key0 + first) & (ps - 1);
                 const unsigned char* const kb = a.kp + ((long long)page * a.kps[0] + (long long)hk * a.kps[1] + (long long)row * a.kps[2]) * ESZ;
@@ -753,7 +857,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
             for (int v = 0; v < 8; ++v) put2(a.part + at * D + 32 * d + 8 * (v >> 1) + 4 * h + 2 * (v & 1), o[d][2 * v], o[d][2 * v + 1]);
         if (h == 0) put2(a.part_ml + at * 2, ref, L);
     }
-    join_splits<D, NT>(a, j, hk, row0, rows);
+    __shared__ int s_last;
+    join_splits<D, NT>(a, j, hk, row0, rows, &s_last);
 }
 
 __global__ __launch_bounds__(256) void clear_words_kernel(unsigned int* w) { w[blockIdx.x * 256 + threadIdx.x] = 0; }
@@ -772,8 +877,8 @@ PagedPlan plan_paged(const ot_paged_attn_params& p, const ot_paged_cache& c) {
     pl.units = c.kv_heads * pl.row_blocks;
     const long long all = (long long)p.batch * pl.units;
     pl.split = p.batch <= kSplitBatch && all <= kCounters;
-    pl.target = pl.rows == 32 || pl.rows == 128 ? 512 : 256;
-    pl.least = pl.rows <= 64 ? 2 : 4;
+    pl.target = pl.rows <= 128 ? 512 : 256;
+    pl.least = pl.rows <= 32 ? 2 : 4;
     const long long tiles = ((long long)c.max_pages * c.page_size + kTile - 1) / kTile + (p.tree_keys + kTile - 1) / kTile;
     const long long most = std::max<long long>(all, pl.target);
     pl.grid = (int)(pl.split ? std::min(most, all * ((tiles + pl.least - 1) / pl.least)) : all);
@@ -798,17 +903,19 @@ int validate_paged(const ot_paged_attn_params* p, const ot_paged_cache* c, bool 
 }
 
 template <int D, bool KV8>
-int launch_paged(const PagedArgs& a, const PagedPlan& pl, hipStream_t s) {
+int launch_paged(const Lead& l, const PagedArgs& a, const PagedPlan& pl, hipStream_t s) {
+#define OT_LEAD_ARGS l.prefix_len, l.table, l.batch, l.units, l.max_pages, l.ps_log2, l.tiles_tree, l.ranges
     constexpr size_t lds = (size_t)2 * 2 * kTile * D * 2;
-    if (pl.rows == 32) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 1>), dim3(pl.grid), dim3(256), 0, s, a);
-    else if (pl.rows == 64) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 2>), dim3(pl.grid), dim3(256), 0, s, a);
+    if (pl.rows == 32) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 1>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
+    else if (pl.rows == 64) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 2>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
     else if (pl.rows == 128) {
         OT_HIP_CHECK(hipFuncSetAttribute((const void*)paged_tiles_kernel<D, KV8, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 4>), dim3(pl.grid), dim3(256), lds, s, a);
+        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 4>), dim3(pl.grid), dim3(256), lds, s, OT_LEAD_ARGS, a);
     } else if constexpr (!(D == 64 && KV8)) {
         OT_HIP_CHECK(hipFuncSetAttribute((const void*)paged_tiles_kernel<D, KV8, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 8>), dim3(pl.grid), dim3(512), lds, s, a);
+        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 8>), dim3(pl.grid), dim3(512), lds, s, OT_LEAD_ARGS, a);
     }
+#undef OT_LEAD_ARGS
     OT_HIP_CHECK(hipGetLastError());
     return OT_OK;
 }
@@ -845,24 +952,24 @@ int ot_tree_verify_attention_paged(const ot_paged_attn_params* p, const ot_paged
     PagedArgs a;
     a.Q = Q; a.Kt = K_tree; a.Vt = V_tree; a.O = O;
     a.kp = (const unsigned char*)cache->k_pages; a.vp = (const unsigned char*)cache->v_pages;
-    a.k_exp = cache->k_exp; a.v_exp = cache->v_exp; a.table = cache->page_table;
-    a.prefix_len = prefix_len; a.mask = mask;
+    a.k_exp = cache->k_exp; a.v_exp = cache->v_exp; a.mask = mask;
     a.sync = (unsigned int*)workspace;
     a.part = (float*)((char*)workspace + OT_PAGED_SYNC_BYTES);
     a.part_ml = a.part + (size_t)pl.grid * pl.slot_rows * cache->head_dim;
-    a.batch = p->batch; a.kv_heads = cache->kv_heads; a.g = p->q_heads / cache->kv_heads; a.n = p->n;
+    a.kv_heads = cache->kv_heads; a.g = p->q_heads / cache->kv_heads; a.n = p->n;
     a.tree_keys = p->tree_keys; a.W = OT_MASK_WORDS(p->tree_keys);
     a.row_blocks = pl.row_blocks; a.units = pl.units;
-    a.num_pages = cache->num_pages; a.max_pages = cache->max_pages; a.ps_log2 = log2_of(cache->page_size);
-    a.split = pl.split; a.target = pl.target; a.least = pl.least; a.slot_rows = pl.slot_rows;
+    a.num_pages = cache->num_pages; a.slot_rows = pl.slot_rows;
+    const Lead lead{prefix_len, cache->page_table, p->batch, pl.units, cache->max_pages, log2_of(cache->page_size),
+                    (p->tree_keys + kTile - 1) / kTile, pl.split ? pl.target << 8 | pl.least : 0};
     a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * kLog2e;
     for (int i = 0; i < 3; ++i) {
         a.qs[i] = p->q_strides[i]; a.kts[i] = p->kt_strides[i]; a.vts[i] = p->vt_strides[i]; a.os[i] = p->o_strides[i];
         a.kps[i] = cache->k_strides[i]; a.vps[i] = cache->v_strides[i];
     }
     hipStream_t s = (hipStream_t)hip_stream;
-    if (cache->dtype == OT_E4M3) return cache->head_dim == 128 ? launch_paged<128, true>(a, pl, s) : launch_paged<64, true>(a, pl, s);
-    return cache->head_dim == 128 ? launch_paged<128, false>(a, pl, s) : launch_paged<64, false>(a, pl, s);
+    if (cache->dtype == OT_E4M3) return cache->head_dim == 128 ? launch_paged<128, true>(lead, a, pl, s) : launch_paged<64, true>(lead, a, pl, s);
+    return cache->head_dim == 128 ? launch_paged<128, false>(lead, a, pl, s) : launch_paged<64, false>(lead, a, pl, s);
 }
 
 }  // extern "C"
