@@ -396,7 +396,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int tr_j = (lane & 15) >> 2, vx = ((lane >> 4) & 1) ^ v_swizzle<D>(tr_j);
     const unsigned short* const v_read = s_v + (4 * h + tr_j) * D + 4 * (lane & 3);
     // probabilities of a block's scores, times V in s_v
-    auto finish = [&](f32x16& s) {
+    auto finish = [&](f32x16& s) __attribute__((always_inline)) {
         u32x4 p[2];
         softmax_block<DB>(s, c, ref, l, o, p);
 #pragma unroll
@@ -697,88 +697,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int ptiles = (j.len + kTile - 1) / kTile;
     const scalar_int table = (scalar_int)l_table + (long long)j.b * l_max_pages;
     const int ps = 1 << l_ps_log2, page_last = max(j.len - 1, 0) >> l_ps_log2;
-    const int tt0 = max(j.t0 - ptiles, 0), tt1 = j.t1 - ptiles;
-    if (tt1 > tt0) union_masks(a, j.b, tt0, tt1, s_union, NT);
     bool bad = false;
+    const int e_wave = wave * (64 / CPM);                // first row of this wavefront's first request; the others NT / CPM rows on
 
-    struct Raw {
-        u32x4 k[CHT], v[CHT];          // a cache tile uses the first CH of each
-        int ke[CH], ve[CH];
-        u64 seen;                      // rows of the tile that exist (V rows that enter the product)
-        u64 mask;                      // tree tile: the words of this lane's query
-    };
-    const int m_row = tid / CPM, m_at = tid % CPM;       // row of the tile and piece of this thread's first request; CH apart NT / CPM rows
-    auto load = [&](int t, Raw& r) {
-        if (t < ptiles) {
-            const int key0 = t * kTile, rem = j.len - key0;
-            r.seen = rem >= kTile ? ~0ull : (1ull << rem) - 1;
-            for (int i = 0; i < kTile >> min(l_ps_log2, 6); ++i) {          // pages of the tile that are none
-                const int k0 = key0 + (i << min(l_ps_log2, 6));
-                if (k0 < j.len && (unsigned)table[k0 >> l_ps_log2] >= (unsigned)a.num_pages) {
-                    bad = true;
-                    const u64 rows_of = ps >= 64 ? ~0ull : ((1ull << (ps & 63)) - 1) << (k0 - key0);
-                    r.seen &= ~rows_of;
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < CH; ++n) {
-                const int first = uniform(wave * (64 / CPM)) + n * (NT / CPM);                    // of the wavefront's rows
-                int page = table[min((key0 + first) >> l_ps_log2, page_last)];
-                page = (unsigned)page < (unsigned)a.num_pages ? page : 0;
-                const int row = (key0 + first) & (ps - 1);
-                const unsigned char* const kb = a.kp + ((long long)page * a.kps[0] + (long long)hk * a.kps[1] + (long long)row * a.kps[2]) * ESZ;
-                const unsigned char* const vb = a.vp + ((long long)page * a.vps[0] + (long long)hk * a.vps[1] + (long long)row * a.vps[2]) * ESZ;
-                r.k[n] = *(const u32x4*)(kb + (unsigned)(lane / CPM) * (unsigned)(a.kps[2] * ESZ) + 16 * m_at);
-                r.v[n] = *(const u32x4*)(vb + (unsigned)(lane / CPM) * (unsigned)(a.vps[2] * ESZ) + 16 * m_at);
-                if constexpr (KV8) {
-                    r.ke[n] = a.k_exp[(long long)page * a.kv_heads + hk];
-                    r.ve[n] = a.v_exp[(long long)page * a.kv_heads + hk];
-                }
-            }
-        } else {
-            const int tt = t - ptiles, last = a.tree_keys - 1;
-            const int rem = a.tree_keys - tt * kTile;
-            const u64 tail = rem >= kTile ? ~0ull : (1ull << rem) - 1;
-            r.seen = s_union[tt - tt0] & tail;
-            r.mask = a.mask[mask_at + tt] & tail;
-            const unsigned short* const kt = (const unsigned short*)a.Kt + (long long)j.b * a.kts[0] + (long long)hk * a.kts[1];
-            const unsigned short* const vt = (const unsigned short*)a.Vt + (long long)j.b * a.vts[0] + (long long)hk * a.vts[1];
-#pragma unroll
-            for (int n = 0; n < CHT; ++n) {
-                const int row = min(tt * kTile + tid / CPR + n * (NT / CPR), last);
-                r.k[n] = *(const u32x4*)(kt + (long long)row * a.kts[2] + 8 * (tid % CPR));
-                r.v[n] = *(const u32x4*)(vt + (long long)row * a.vts[2] + 8 * (tid % CPR));
-            }
-        }
-    };
-    auto stage = [&](int t, Raw& r, int buf) {
-        unsigned short* const sk = s_kv + buf * BUF;
-        unsigned short* const sv = sk + kTile * D;
-        if (KV8 && t < ptiles) {
-#pragma unroll
-            for (int n = 0; n < CH; ++n) {
-                const int row = m_row + n * (NT / CPM);
-                u32x4 lo, hi, w = r.v[n];
-                widen16(r.k[n], exp_scale(r.ke[n]), lo, hi);
-                *(u32x4*)(sk + row * D + (((2 * m_at) ^ (row & (CPR - 1))) << 3)) = lo;
-                *(u32x4*)(sk + row * D + (((2 * m_at + 1) ^ (row & (CPR - 1))) << 3)) = hi;
-                if (r.seen != ~0ull && !(r.seen >> row & 1)) w = u32x4{0, 0, 0, 0};
-                widen16(w, exp_scale(r.ve[n]), lo, hi);
-                u32x4* const to = (u32x4*)(sv + row * D + ((m_at ^ v_swizzle<D>(row)) << 4));
-                to[0] = lo; to[1] = hi;
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < CHT; ++n) {
-                const int row = tid / CPR + n * (NT / CPR), at = tid % CPR;
-                u32x4 w = r.v[n];
-                *(u32x4*)(sk + row * D + ((at ^ (row & (CPR - 1))) << 3)) = r.k[n];
-                if (r.seen != ~0ull && !(r.seen >> row & 1)) w = u32x4{0, 0, 0, 0};
-                *(u32x4*)(sv + row * D + (((at >> 1) ^ v_swizzle<D>(row)) << 4) + 8 * (at & 1)) = w;
-            }
-        }
-    };
-    auto compute = [&](int t, u64 visible, int buf) {
+    auto put_k = [&](unsigned short* sk, int row, int piece, const u32x4& w) { *(u32x4*)(sk + row * D + ((piece ^ (row & (CPR - 1))) << 3)) = w; };
+    auto compute = [&](int buf, bool all, u64 visible) __attribute__((always_inline)) {
         const unsigned short* const sk = s_kv + buf * BUF;
         const unsigned short* const sv = sk + kTile * D;
         u32x4 p[2][2];
@@ -793,7 +716,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kb], 0, 0, 0);
             }
         }
-        if (t >= ptiles || visible != ~0ull) {
+        if (!all) {
             hide(s[0], (unsigned)visible, h);
             hide(s[1], (unsigned)(visible >> 32), h);
         }
@@ -810,26 +733,135 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
     };
 
-    if (j.t0 < j.t1) {
-        Raw ra, rb_;
-        u64 vis[2];
-        auto visible_of = [&](int t, const Raw& r) { return t < ptiles ? r.seen : r.mask; };
-        load(j.t0, ra);
-        if (j.t0 + 1 < j.t1) load(j.t0 + 1, rb_);
-        stage(j.t0, ra, 0);
-        vis[0] = visible_of(j.t0, ra);
+    // ---- cache ----
+    const int tp1 = min(j.t1, ptiles);
+    int buf = 0;
+    if (j.t0 < tp1) {
+        struct Pages {
+            int page[4];                   // of the tile's four times sixteen rows
+            u64 seen;                      // its rows that exist
+        };
+        auto in_range = [&](int t) { return min(t, tp1 - 1); };
+        auto pages_of = [&](int t) {
+            Pages r;
+            const int key0 = t * kTile, rem = j.len - key0;
+            r.seen = rem >= kTile ? ~0ull : (1ull << rem) - 1;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r.page[e] = table[min((key0 + 16 * e) >> l_ps_log2, page_last)];
+            return r;
+        };
+        u32x4 kr[2][CH], vr[2][CH];
+        int ke[2][CH], ve[2][CH];
+        u64 seen[2];
+        const unsigned k_lane = (unsigned)(lane / CPM) * (unsigned)(a.kps[2] * ESZ) + 16 * (lane % CPM);
+        const unsigned v_lane = (unsigned)(lane / CPM) * (unsigned)(a.vps[2] * ESZ) + 16 * (lane % CPM);
+        auto load = [&](int t, Pages r, int at) {        // past the last tile: that one again (a load under a condition makes waits longer)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if ((unsigned)r.page[e] >= (unsigned)a.num_pages) {
+                    if (t * kTile + 16 * e < j.len) bad = true;
+                    r.page[e] = 0;
+                    r.seen &= ~(0xffffull << (16 * e));
+                }
+            seen[at] = r.seen;
+#pragma unroll
+            for (int n = 0; n < CH; ++n) {
+                const int first = e_wave + n * (NT / CPM), e = first >> 4;       // rows first .. first + 64 / CPM - 1
+                const int page = e == 0 ? r.page[0] : e == 1 ? r.page[1] : e == 2 ? r.page[2] : r.page[3];
+                const int row = (t * kTile + first) & (ps - 1);
+                const unsigned char* const kb = a.kp + ((long long)page * a.kps[0] + (long long)hk * a.kps[1] + (long long)row * a.kps[2]) * ESZ;
+                const unsigned char* const vb = a.vp + ((long long)page * a.vps[0] + (long long)hk * a.vps[1] + (long long)row * a.vps[2]) * ESZ;
+                kr[at][n] = *(const u32x4*)(kb + k_lane);
+                vr[at][n] = *(const u32x4*)(vb + v_lane);
+                if constexpr (KV8) {
+                    ke[at][n] = a.k_exp[(long long)page * a.kv_heads + hk];
+                    ve[at][n] = a.v_exp[(long long)page * a.kv_heads + hk];
+                }
+            }
+        };
+        auto stage = [&](int at, int to) {
+            unsigned short* const sk = s_kv + to * BUF;
+            unsigned short* const sv = sk + kTile * D;
+#pragma unroll
+            for (int n = 0; n < CH; ++n) {
+                const int row = tid / CPM + n * (NT / CPM), piece = tid % CPM;
+                u32x4 w = vr[at][n];
+                if (seen[at] != ~0ull && !(seen[at] >> row & 1)) w = u32x4{0, 0, 0, 0};
+                if constexpr (KV8) {
+                    u32x4 lo, hi;
+                    widen16(kr[at][n], exp_scale(ke[at][n]), lo, hi);
+                    put_k(sk, row, 2 * piece, lo);
+                    put_k(sk, row, 2 * piece + 1, hi);
+                    widen16(w, exp_scale(ve[at][n]), lo, hi);
+                    u32x4* const v = (u32x4*)(sv + row * D + ((piece ^ v_swizzle<D>(row)) << 4));
+                    v[0] = lo; v[1] = hi;
+                } else {
+                    put_k(sk, row, piece, kr[at][n]);
+                    *(u32x4*)(sv + row * D + (((piece >> 1) ^ v_swizzle<D>(row)) << 4) + 8 * (piece & 1)) = w;
+                }
+            }
+        };
         int t = j.t0;
-        while (true) {                                   // tile t is staged in buffer 0, tile t + 1 on its way in rb_
+        load(t, pages_of(t), 0);
+        load(in_range(t + 1), pages_of(in_range(t + 1)), 1);
+        Pages ahead = pages_of(in_range(t + 2));
+        u64 now = seen[0];
+        stage(0, 0);
+        // tile t is in buffer AT, tile t + 1 in registers 1 - AT; true: there is another one
+        auto step = [&](auto at_c) {
+            constexpr int at = at_c;
             __syncthreads();
-            if (t + 2 < j.t1) load(t + 2, ra);
-            if (t + 1 < j.t1) { stage(t + 1, rb_, 1); vis[1] = visible_of(t + 1, rb_); }
-            compute(t, vis[0], 0);
-            if (++t >= j.t1) break;
+            const Pages after = pages_of(in_range(t + 3));
+            load(in_range(t + 2), ahead, at);
+            ahead = after;
+            const u64 next = seen[1 - at];
+            stage(1 - at, 1 - at);
+            compute(at, now == ~0ull, now);
+            now = next;
+            return ++t < tp1;
+        };
+        while (step(std::integral_constant<int, 0>()) && step(std::integral_constant<int, 1>())) {}
+        buf = (tp1 - j.t0) & 1;                          // (the other one is still being read, this one holds a copy of the last tile)
+    }
+
+    // ---- tree ----
+    {
+        const int tt0 = max(j.t0 - ptiles, 0), tt1 = j.t1 - ptiles, last = a.tree_keys - 1;
+        const unsigned short* const kt = (const unsigned short*)a.Kt + (long long)j.b * a.kts[0] + (long long)hk * a.kts[1];
+        const unsigned short* const vt = (const unsigned short*)a.Vt + (long long)j.b * a.vts[0] + (long long)hk * a.vts[1];
+        u32x4 kr[CHT], vr[CHT];
+        u64 mask = 0, next = 0;
+        auto load = [&](int tt) {
+            next = a.mask[mask_at + tt];
+#pragma unroll
+            for (int n = 0; n < CHT; ++n) {
+                const int row = min(tt * kTile + tid / CPR + n * (NT / CPR), last);
+                kr[n] = *(const u32x4*)(kt + (long long)row * a.kts[2] + 8 * (tid % CPR));
+                vr[n] = *(const u32x4*)(vt + (long long)row * a.vts[2] + 8 * (tid % CPR));
+            }
+        };
+        if (tt1 > tt0) {
+            load(tt0);
+            union_masks(a, j.b, tt0, tt1, s_union, NT);
+        }
+        for (int tt = tt0; tt < tt1; ++tt) {
+            const int rem = a.tree_keys - tt * kTile;
+            const u64 tail = rem >= kTile ? ~0ull : (1ull << rem) - 1, any = s_union[tt - tt0] & tail;
+            unsigned short* const sk = s_kv + buf * BUF;
+            unsigned short* const sv = sk + kTile * D;
+#pragma unroll
+            for (int n = 0; n < CHT; ++n) {
+                const int row = tid / CPR + n * (NT / CPR), piece = tid % CPR;
+                u32x4 w = vr[n];
+                put_k(sk, row, piece, kr[n]);
+                if (!(any >> row & 1)) w = u32x4{0, 0, 0, 0};
+                *(u32x4*)(sv + row * D + (((piece >> 1) ^ v_swizzle<D>(row)) << 4) + 8 * (piece & 1)) = w;
+            }
+            mask = next & tail;
             __syncthreads();
-            if (t + 2 < j.t1) load(t + 2, rb_);
-            if (t + 1 < j.t1) { stage(t + 1, ra, 0); vis[0] = visible_of(t + 1, ra); }
-            compute(t, vis[1], 1);
-            if (++t >= j.t1) break;
+            load(min(tt + 1, tt1 - 1));
+            compute(buf, false, mask);
+            buf ^= 1;
         }
     }
     if (bad && lane == 0)
