@@ -207,15 +207,15 @@ __device__ __forceinline__ bf16x8 column_of_8_rows(const unsigned short* seg, in
 // 32-byte slots of a 256-byte window.
 template <int D> __device__ __forceinline__ int v_swizzle(int r) { return D == 128 ? (r & 3) << 1 : ((r >> 1) & 1) << 1; }
 
-// A 32-key block of scores (lane: query l32, keys 8 (v/4) + 4 h + v%4) becomes probabilities; returns them packed as the
-// B operands of the two 16-key slabs, and rescales what the row has summed when the reference moves.
-template <int NO>
-__device__ __forceinline__ void softmax_block(f32x16& s, float c, float& ref, float& l, f32x16 (&o)[NO], u32x4 (&p)[2]) {
+// NB 32-key blocks of scores (lane: query l32, keys 8 (v/4) + 4 h + v%4 of a block) become probabilities; returns them packed as the
+// B operands of the blocks' 16-key slabs, and rescales what the row has summed when the reference moves.
+template <int NB, int NO>
+__device__ __forceinline__ void softmax_blocks(f32x16 (&s)[NB], float c, float& ref, float& l, f32x16 (&o)[NO], u32x4 (&p)[2 * NB]) {
     // (compiler-made maxima: an assembly one would not wait for the matrix instruction that makes its operand)
-    float m = fmaxf(fmaxf(s[0], s[1]), s[2]);
+    float m = s[0][0];
 #pragma unroll
-    for (int v = 3; v < 15; v += 2) m = fmaxf(fmaxf(m, s[v]), s[v + 1]);
-    m = xhalf_max(fmaxf(m, s[15])) * c;
+    for (int i = 1; i + 1 < 16 * NB; i += 2) m = fmaxf(fmaxf(m, s[i / 16][i % 16]), s[(i + 1) / 16][(i + 1) % 16]);
+    m = xhalf_max(fmaxf(m, s[NB - 1][15])) * c;
     if (__any(m > ref + kSlack)) {
         const float to = m > ref + kSlack ? m : ref, f = __builtin_amdgcn_exp2f(ref - to);
         l *= f;
@@ -225,17 +225,39 @@ __device__ __forceinline__ void softmax_block(f32x16& s, float c, float& ref, fl
             for (int v = 0; v < 16; ++v) o[d][v] *= f;
         ref = to;
     }
-    float sum = 0.f;
+    float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-        s[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c, -ref));
-        sum += s[v];
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            s[i][v] = __builtin_amdgcn_exp2f(fmaf(s[i][v], c, -ref));
+            sum[v & 1] += s[i][v];
+        }
+    l += sum[0] + sum[1];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[2 * i + u][e] = pack_bf16(s[i][8 * u + 2 * e], s[i][8 * u + 2 * e + 1]);
+}
+// STEPS products whose operands come from LDS, each requested AHEAD products before it is needed and held in that order (left to
+// itself the compiler reads an operand right before its product, and every product waits for LDS).  read(i) returns the
+// operands of product i, multiply(i, operands) does it; i is a constant in both.
+template <int STEPS, int AHEAD, typename Read, typename Multiply>
+__device__ __forceinline__ void pipelined(Read read, Multiply multiply) {
+    decltype(read(0)) ring[AHEAD + 1];
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) ring[i] = read(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+        if (i + AHEAD < STEPS) ring[(i + AHEAD) % (AHEAD + 1)] = read(i + AHEAD);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(i, ring[i % (AHEAD + 1)]);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    l += sum;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[u][i] = pack_bf16(s[8 * u + 2 * i], s[8 * u + 2 * i + 1]);
 }
 // scores of keys whose bit is not set
 __device__ __forceinline__ void hide(f32x16& s, unsigned bits, int h) {
@@ -396,9 +418,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int tr_j = (lane & 15) >> 2, vx = ((lane >> 4) & 1) ^ v_swizzle<D>(tr_j);
     const unsigned short* const v_read = s_v + (4 * h + tr_j) * D + 4 * (lane & 3);
     // probabilities of a block's scores, times V in s_v
-    auto finish = [&](f32x16& s) __attribute__((always_inline)) {
+    auto finish = [&](f32x16& score) __attribute__((always_inline)) {
         u32x4 p[2];
-        softmax_block<DB>(s, c, ref, l, o, p);
+        f32x16 s[1] = {score};
+        softmax_blocks(s, c, ref, l, o, p);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -666,9 +689,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     constexpr int CH = kTile * CPM / NT;               // pieces of K per thread and tile, and of V
     constexpr int CHT = kTile * CPR / NT;              // the same of a tree tile
     static_assert(CH >= 1 && 64 / CPM <= 16, "a piece per thread; a wavefront's rows lie in one page");
-    extern __shared__ __attribute__((aligned(16))) unsigned short s_kv[];       // [2][K, V][64][D]
+    extern __shared__ __attribute__((aligned(16))) unsigned short s_kv[];       // tiles [64][D]
     __shared__ u64 s_union[OT_MAX_TREE_KEYS / 64];
-    constexpr int BUF = 2 * kTile * D;
+    constexpr bool TURNS = NW == 8;                    // two wavefronts of a SIMD take turns, see below
+    constexpr int TILE = kTile * D;                    // a tile of K or of V in LDS
+    auto k_buf = [&](int i) { return s_kv + i * TILE; };                         // two of K,
+    auto v_buf = [&](int i) { return s_kv + (2 + i) * TILE; };                   // two of V, three if the wavefronts take turns
     const Job j = find_job(OT_LEAD, a.sync, blockIdx.x);
     if (j.none) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, h = lane >> 5;
@@ -701,41 +727,49 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int e_wave = wave * (64 / CPM);                // first row of this wavefront's first request; the others NT / CPM rows on
 
     auto put_k = [&](unsigned short* sk, int row, int piece, const u32x4& w) { *(u32x4*)(sk + row * D + ((piece ^ (row & (CPR - 1))) << 3)) = w; };
-    auto compute = [&](int buf, bool all, u64 visible) __attribute__((always_inline)) {
-        const unsigned short* const sk = s_kv + buf * BUF;
-        const unsigned short* const sv = sk + kTile * D;
-        u32x4 p[2][2];
-        f32x16 s[2];
+    auto k_frag = [&](const unsigned short* sk, int kb, int i) {
+        return __builtin_bit_cast(bf16x8, *(const u32x4*)(sk + (32 * kb + l32) * D + (((2 * i + h) ^ kx) << 3)));
+    };
+    auto v_frag = [&](const unsigned short* sv, int u, int d) {
+        return column_of_8_rows(sv + (16 * u + 4 * h + tr_j) * D + (((2 * d) ^ vx) << 4) + 4 * (lane & 3), 8 * D);
+    };
+    f32x16 s[2];
+    u32x4 p[4];
+    auto clear_scores = [&] {
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
-#pragma unroll
-            for (int i = 0; i < SL; ++i) {
-                const bf16x8 kf = __builtin_bit_cast(bf16x8, *(const u32x4*)(sk + (32 * kb + l32) * D + (((2 * i + h) ^ kx) << 3)));
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[i], s[kb], 0, 0, 0);
-            }
-        }
-        if (!all) {
+        for (int v = 0; v < 16; ++v) s[0][v] = s[1][v] = 0.f;
+    };
+    auto scores = [&](const unsigned short* sk) __attribute__((always_inline)) {
+        clear_scores();
+        pipelined<2 * SL, 4>([&](int i) { return k_frag(sk, i & 1, i >> 1); },
+                             [&](int i, const bf16x8& k) { s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qf[i >> 1], s[i & 1], 0, 0, 0); });
+    };
+    auto weights = [&](u64 visible) __attribute__((always_inline)) {
+        if (visible != ~0ull) {
             hide(s[0], (unsigned)visible, h);
             hide(s[1], (unsigned)(visible >> 32), h);
         }
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            softmax_block<DB>(s[kb], c, ref, l, o, p[kb]);
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int d = 0; d < DB; ++d) {
-                    const bf16x8 vf = column_of_8_rows(sv + (32 * kb + 16 * u + 4 * h + tr_j) * D + (((2 * d) ^ vx) << 4) + 4 * (lane & 3), 8 * D);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, p[kb][u]), o[d], 0, 0, 0);
-                }
-        }
+        softmax_blocks(s, c, ref, l, o, p);
+    };
+    auto add_value = [&](int i, const bf16x8& v) __attribute__((always_inline)) {
+        o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, p[i / DB]), o[i % DB], 0, 0, 0);
+    };
+    auto values = [&](const unsigned short* sv) __attribute__((always_inline)) {
+        pipelined<4 * DB, 3>([&](int i) { return v_frag(sv, i / DB, i % DB); }, add_value);
+    };
+    // values of one tile and scores of the next, 4 DB = 2 SL of either
+    auto values_and_scores = [&](const unsigned short* sv, const unsigned short* sk) __attribute__((always_inline)) {
+        struct Pair { bf16x8 v, k; };
+        clear_scores();
+        pipelined<2 * SL, 2>([&](int i) { return Pair{v_frag(sv, i / DB, i % DB), k_frag(sk, i & 1, i >> 1)}; },
+                             [&](int i, const Pair& x) {
+                                 add_value(i, x.v);
+                                 s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x.k, qf[i >> 1], s[i & 1], 0, 0, 0);
+                             });
     };
 
     // ---- cache ----
     const int tp1 = min(j.t1, ptiles);
-    int buf = 0;
     if (j.t0 < tp1) {
         struct Pages {
             int page[4];                   // of the tile's four times sixteen rows
@@ -750,12 +784,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
             for (int e = 0; e < 4; ++e) r.page[e] = table[min((key0 + 16 * e) >> l_ps_log2, page_last)];
             return r;
         };
-        u32x4 kr[2][CH], vr[2][CH];
-        int ke[2][CH], ve[2][CH];
-        u64 seen[2];
+        u32x4 kr[CH], vr[CH];
+        int ke[CH], ve[CH];
+        u64 next = 0;                      // rows of the tile in registers that exist
         const unsigned k_lane = (unsigned)(lane / CPM) * (unsigned)(a.kps[2] * ESZ) + 16 * (lane % CPM);
         const unsigned v_lane = (unsigned)(lane / CPM) * (unsigned)(a.vps[2] * ESZ) + 16 * (lane % CPM);
-        auto load = [&](int t, Pages r, int at) {        // past the last tile: that one again (a load under a condition makes waits longer)
+        auto load = [&](int t, Pages r) {        // past the last tile: that one again (a load under a condition makes waits longer)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if ((unsigned)r.page[e] >= (unsigned)a.num_pages) {
@@ -763,7 +797,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
                     r.page[e] = 0;
                     r.seen &= ~(0xffffull << (16 * e));
                 }
-            seen[at] = r.seen;
+            next = r.seen;
 #pragma unroll
             for (int n = 0; n < CH; ++n) {
                 const int first = e_wave + n * (NT / CPM), e = first >> 4;       // rows first .. first + 64 / CPM - 1
@@ -771,57 +805,83 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 const int row = (t * kTile + first) & (ps - 1);
                 const unsigned char* const kb = a.kp + ((long long)page * a.kps[0] + (long long)hk * a.kps[1] + (long long)row * a.kps[2]) * ESZ;
                 const unsigned char* const vb = a.vp + ((long long)page * a.vps[0] + (long long)hk * a.vps[1] + (long long)row * a.vps[2]) * ESZ;
-                kr[at][n] = *(const u32x4*)(kb + k_lane);
-                vr[at][n] = *(const u32x4*)(vb + v_lane);
+                kr[n] = *(const u32x4*)(kb + k_lane);
+                vr[n] = *(const u32x4*)(vb + v_lane);
                 if constexpr (KV8) {
-                    ke[at][n] = a.k_exp[(long long)page * a.kv_heads + hk];
-                    ve[at][n] = a.v_exp[(long long)page * a.kv_heads + hk];
+                    ke[n] = a.k_exp[(long long)page * a.kv_heads + hk];
+                    ve[n] = a.v_exp[(long long)page * a.kv_heads + hk];
                 }
             }
         };
-        auto stage = [&](int at, int to) {
-            unsigned short* const sk = s_kv + to * BUF;
-            unsigned short* const sv = sk + kTile * D;
+        auto stage = [&](unsigned short* sk, unsigned short* sv) {
 #pragma unroll
             for (int n = 0; n < CH; ++n) {
                 const int row = tid / CPM + n * (NT / CPM), piece = tid % CPM;
-                u32x4 w = vr[at][n];
-                if (seen[at] != ~0ull && !(seen[at] >> row & 1)) w = u32x4{0, 0, 0, 0};
+                u32x4 w = vr[n];
+                if (next != ~0ull && !(next >> row & 1)) w = u32x4{0, 0, 0, 0};
                 if constexpr (KV8) {
                     u32x4 lo, hi;
-                    widen16(kr[at][n], exp_scale(ke[at][n]), lo, hi);
+                    widen16(kr[n], exp_scale(ke[n]), lo, hi);
                     put_k(sk, row, 2 * piece, lo);
                     put_k(sk, row, 2 * piece + 1, hi);
-                    widen16(w, exp_scale(ve[at][n]), lo, hi);
+                    widen16(w, exp_scale(ve[n]), lo, hi);
                     u32x4* const v = (u32x4*)(sv + row * D + ((piece ^ v_swizzle<D>(row)) << 4));
                     v[0] = lo; v[1] = hi;
                 } else {
-                    put_k(sk, row, piece, kr[at][n]);
+                    put_k(sk, row, piece, kr[n]);
                     *(u32x4*)(sv + row * D + (((piece >> 1) ^ v_swizzle<D>(row)) << 4) + 8 * (piece & 1)) = w;
                 }
             }
         };
-        int t = j.t0;
-        load(t, pages_of(t), 0);
-        load(in_range(t + 1), pages_of(in_range(t + 1)), 1);
-        Pages ahead = pages_of(in_range(t + 2));
-        u64 now = seen[0];
-        stage(0, 0);
-        // tile t is in buffer AT, tile t + 1 in registers 1 - AT; true: there is another one
-        auto step = [&](auto at_c) {
-            constexpr int at = at_c;
-            __syncthreads();
-            const Pages after = pages_of(in_range(t + 3));
-            load(in_range(t + 2), ahead, at);
-            ahead = after;
-            const u64 next = seen[1 - at];
-            stage(1 - at, 1 - at);
-            compute(at, now == ~0ull, now);
-            now = next;
-            return ++t < tp1;
+        load(j.t0, pages_of(j.t0));
+        Pages ahead = pages_of(in_range(j.t0 + 1));
+        int x = j.t0;                                    // tile in registers
+        u64 staged = 0, before = 0;                      // `next` of the last tile that was staged, and of the one before it
+        int vb = 0;                                      // V buffer of tile x
+        auto advance = [&]() __attribute__((always_inline)) {                    // tile x to LDS, tile x + 1 on its way
+            stage(k_buf((x - j.t0) & 1), v_buf(vb));
+            before = staged;
+            staged = next;
+            ++x;
+            load(in_range(x), ahead);
+            ahead = pages_of(in_range(x + 1));
+            vb = vb == (TURNS ? 2 : 1) ? 0 : vb + 1;
         };
-        while (step(std::integral_constant<int, 0>()) && step(std::integral_constant<int, 1>())) {}
-        buf = (tp1 - j.t0) & 1;                          // (the other one is still being read, this one holds a copy of the last tile)
+        advance();
+        if constexpr (TURNS) {
+            // The two wavefronts of a SIMD take turns: while wavefronts 0..3 have the matrix cores (values of tile t - 1, scores
+            // of tile t), wavefronts 4..7 do the exponentials of tile t - 1 and bring a tile into LDS, and the other way
+            // round; a barrier changes sides.  A tile of V is read half a turn into the next tile and written two turns
+            // ahead: three buffers; K two.  Without turns both wavefronts would be at the same kind of work, since they meet
+            // at every tile: 16 x 32 heads x 256 nodes over 8192 keys 607 us, not OT_TURNS us.
+            const bool second = wave >= 4;
+            __syncthreads();
+            if (second) { advance(); __syncthreads(); }
+            int va = 0;                                  // V buffer of tile t
+            scores(k_buf(0));
+            for (int t = j.t0;;) {
+                __syncthreads();
+                const u64 visible = second ? before : staged;
+                advance();                               // (past the last tile: a copy of it, which nobody reads)
+                weights(visible);
+                __syncthreads();
+                if (++t >= tp1) break;
+                values_and_scores(v_buf(va), k_buf((t - j.t0) & 1));
+                va = va == 2 ? 0 : va + 1;
+            }
+            if (!second) __syncthreads();
+            values(v_buf(va));
+        } else {
+            for (int t = j.t0; t < tp1; ++t) {
+                const int now = (t - j.t0) & 1;
+                __syncthreads();
+                const u64 visible = staged;
+                advance();
+                scores(k_buf(now));
+                weights(visible);
+                values(v_buf(now));
+            }
+        }
     }
 
     // ---- tree ----
@@ -830,7 +890,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         const unsigned short* const kt = (const unsigned short*)a.Kt + (long long)j.b * a.kts[0] + (long long)hk * a.kts[1];
         const unsigned short* const vt = (const unsigned short*)a.Vt + (long long)j.b * a.vts[0] + (long long)hk * a.vts[1];
         u32x4 kr[CHT], vr[CHT];
-        u64 mask = 0, next = 0;
+        u64 next = 0;
+        int buf = 0;
         auto load = [&](int tt) {
             next = a.mask[mask_at + tt];
 #pragma unroll
@@ -847,8 +908,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         for (int tt = tt0; tt < tt1; ++tt) {
             const int rem = a.tree_keys - tt * kTile;
             const u64 tail = rem >= kTile ? ~0ull : (1ull << rem) - 1, any = s_union[tt - tt0] & tail;
-            unsigned short* const sk = s_kv + buf * BUF;
-            unsigned short* const sv = sk + kTile * D;
+            unsigned short* const sk = k_buf(buf);
+            unsigned short* const sv = v_buf(buf);
 #pragma unroll
             for (int n = 0; n < CHT; ++n) {
                 const int row = tid / CPR + n * (NT / CPR), piece = tid % CPR;
@@ -857,10 +918,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 if (!(any >> row & 1)) w = u32x4{0, 0, 0, 0};
                 *(u32x4*)(sv + row * D + (((piece >> 1) ^ v_swizzle<D>(row)) << 4) + 8 * (piece & 1)) = w;
             }
-            mask = next & tail;
+            const u64 mask = next & tail;
             __syncthreads();
             load(min(tt + 1, tt1 - 1));
-            compute(buf, false, mask);
+            scores(sk);
+            weights(mask);
+            values(sv);
             buf ^= 1;
         }
     }
@@ -937,15 +1000,15 @@ int validate_paged(const ot_paged_attn_params* p, const ot_paged_cache* c, bool 
 template <int D, bool KV8>
 int launch_paged(const Lead& l, const PagedArgs& a, const PagedPlan& pl, hipStream_t s) {
 #define OT_LEAD_ARGS l.prefix_len, l.table, l.batch, l.units, l.max_pages, l.ps_log2, l.tiles_tree, l.ranges
-    constexpr size_t lds = (size_t)2 * 2 * kTile * D * 2;
+    constexpr size_t tile = (size_t)kTile * D * 2;
     if (pl.rows == 32) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 1>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
     else if (pl.rows == 64) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 2>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
     else if (pl.rows == 128) {
-        OT_HIP_CHECK(hipFuncSetAttribute((const void*)paged_tiles_kernel<D, KV8, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 4>), dim3(pl.grid), dim3(256), lds, s, OT_LEAD_ARGS, a);
+        OT_HIP_CHECK(hipFuncSetAttribute((const void*)paged_tiles_kernel<D, KV8, 4>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(4 * tile)));
+        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 4>), dim3(pl.grid), dim3(256), 4 * tile, s, OT_LEAD_ARGS, a);
     } else if constexpr (!(D == 64 && KV8)) {
-        OT_HIP_CHECK(hipFuncSetAttribute((const void*)paged_tiles_kernel<D, KV8, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 8>), dim3(pl.grid), dim3(512), lds, s, OT_LEAD_ARGS, a);
+        OT_HIP_CHECK(hipFuncSetAttribute((const void*)paged_tiles_kernel<D, KV8, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)(5 * tile)));
+        hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 8>), dim3(pl.grid), dim3(512), 5 * tile, s, OT_LEAD_ARGS, a);
     }
 #undef OT_LEAD_ARGS
     OT_HIP_CHECK(hipGetLastError());
