@@ -400,7 +400,7 @@ typedef struct ot_paged_cache {
     int32_t max_pages;                  /* entries per sequence in page_table; max_pages * page_size < 2^30 */
     int64_t k_strides[3], v_strides[3]; /* page, head, row; elements */
     void *k_pages, *v_pages;            /* device */
-    uint8_t *k_exp, *v_exp;             /* device [num_pages][kv_heads], OT_E4M3 only */
+    uint8_t *k_exp, *v_exp;             /* device [num_pages][kv_heads], 4-byte aligned (read in aligned words of 4), OT_E4M3 only */
     const int32_t* page_table;          /* device [batch][max_pages] */
 } ot_paged_cache;
 

@@ -24,7 +24,7 @@ inline int validate_cache(const ot_paged_cache* c, bool pointers) {
     if (!pointers) return OT_OK;
     if (!c->k_pages || !c->v_pages || !c->page_table) return OT_ERR_INVALID_ARG;
     if ((uintptr_t)c->k_pages % 16 || (uintptr_t)c->v_pages % 16 || (uintptr_t)c->page_table % 4) return OT_ERR_INVALID_ARG;
-    if (c->dtype == OT_E4M3 && (!c->k_exp || !c->v_exp)) return OT_ERR_INVALID_ARG;
+    if (c->dtype == OT_E4M3 && (!c->k_exp || !c->v_exp || (uintptr_t)c->k_exp % 4 || (uintptr_t)c->v_exp % 4)) return OT_ERR_INVALID_ARG;
     return OT_OK;
 }
 

@@ -31,6 +31,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 // Page numbers are read through the scalar cache (nothing writes the table while a call runs): as vector loads they would
 // queue behind the K and V rows in flight, and waiting for one would wait for all of those.
 typedef const int32_t __attribute__((address_space(4))) * scalar_int;
+// The byte at p (the same p in all lanes), likewise: a scalar load has at least four bytes, those of the aligned word around it.
+__device__ __forceinline__ int scalar_byte(const unsigned char* p) {
+    return *(scalar_int)((uintptr_t)p & ~(uintptr_t)3) >> (8 * ((uintptr_t)p & 3)) & 255;
+}
 constexpr int kCounters = OT_PAGED_SYNC_BYTES / 4 - 1024;   // tickets, behind the kilo-word that ends with the status word
 constexpr int kSplitBatch = 256;                             // sequences of a batch whose contexts are cut into ranges
 constexpr int kTile = 64;
@@ -234,6 +238,7 @@ __device__ __forceinline__ void softmax_blocks(f32x16 (&s)[NB], float c, float& 
             sum[v & 1] += s[i][v];
         }
     l += sum[0] + sum[1];
+    asm volatile("" : "+v"(l));                          // (here, not after the next products)
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -463,7 +468,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     };
     constexpr int DIST = 1;         // blocks requested ahead
     u32x4 kr[DIST][KL], vr[DIST][KL];
-    int ke[DIST], ve[DIST][2];                           // exponents: of this lane's key, of either half of the block
+    int ke[DIST][2], ve[DIST][2];                        // exponents of either half of the block
     // Every instruction asks for whole rows, and says that they are read once: 16 bytes of 32 rows each instead, as the matrix
     // operand wants them, or without the hint, 64 heads over 4 x 100000 keys take 172 us, not 156.
     const unsigned k_lane = (unsigned)(lane / CPR) * (unsigned)(a.kps[2] * ESZ) + 16 * (lane % CPR);
@@ -474,7 +479,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const unsigned char* b[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) b[e] = kh + ((long long)r.page[e] * a.kps[0] + (long long)((32 * i + 16 * e) & (ps - 1)) * a.kps[2]) * ESZ;
-        if constexpr (KV8) ke[at] = a.k_exp[(long long)(l32 & 16 ? r.page[1] : r.page[0]) * a.kv_heads + hk];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if constexpr (KV8) ke[at][e] = scalar_byte(a.k_exp + ((long long)r.page[e] * a.kv_heads + hk));
 #pragma unroll
         for (int n = 0; n < KL; ++n)                     // rows n RPL .. n RPL + RPL - 1 of the block
             kr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + (long long)((n * RPL) & 15) * a.kps[2] * ESZ + k_lane));
@@ -484,7 +491,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             b[e] = vh + ((long long)r.page[e] * a.vps[0] + (long long)((32 * i + 16 * e) & (ps - 1)) * a.vps[2]) * ESZ;
-            if constexpr (KV8) ve[at][e] = a.v_exp[(long long)r.page[e] * a.kv_heads + hk];
+            if constexpr (KV8) ve[at][e] = scalar_byte(a.v_exp + ((long long)r.page[e] * a.kv_heads + hk));
         }
 #pragma unroll
         for (int n = 0; n < KL; ++n)
@@ -511,11 +518,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         }
         wave_fence();
     };
-    auto scores = [&](int e) {                           // e: exponent of this lane's key
+    auto scores = [&](int e0, int e1) {                  // exponents of the block's halves
         f32x16 s;
 #pragma unroll
         for (int v = 0; v < 16; ++v) s[v] = 0.f;
-        const float f = KV8 ? exp_scale(e) : 1.f;
+        const float f = KV8 ? (l32 & 16 ? exp_scale(e1) : exp_scale(e0)) : 1.f;
 #pragma unroll
         for (int i = 0; i < NJ; ++i) {
             u32x4 lo, hi;
@@ -554,13 +561,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 const Pages after = pages_of(in_range(i + DIST * KS + KS));
                 check(to, ahead);
                 const unsigned now = seen[slot];
-                const int e = KV8 ? ke[slot] : 0;
+                const int e0 = KV8 ? ke[slot][0] : 0, e1 = KV8 ? ke[slot][1] : 0;
                 stage(now, slot);
                 __builtin_amdgcn_sched_barrier(0);
                 load_v(to, ahead, slot);
                 load_k(to, ahead, slot);
                 __builtin_amdgcn_sched_barrier(0);
-                f32x16 s = scores(e);
+                f32x16 s = scores(e0, e1);
                 if (now != 0xffffffffu) hide(s, now, h);
                 finish(s);
                 seen[slot] = ahead.seen;
@@ -808,8 +815,8 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 kr[n] = *(const u32x4*)(kb + k_lane);
                 vr[n] = *(const u32x4*)(vb + v_lane);
                 if constexpr (KV8) {
-                    ke[n] = a.k_exp[(long long)page * a.kv_heads + hk];
-                    ve[n] = a.v_exp[(long long)page * a.kv_heads + hk];
+                    ke[n] = scalar_byte(a.k_exp + ((long long)page * a.kv_heads + hk));
+                    ve[n] = scalar_byte(a.v_exp + ((long long)page * a.kv_heads + hk));
                 }
             }
         };
