@@ -31,11 +31,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 // Page numbers are read through the scalar cache (nothing writes the table while a call runs): as vector loads they would
 // queue behind the K and V rows in flight, and waiting for one would wait for all of those.
 typedef const int32_t __attribute__((address_space(4))) * scalar_int;
-// The byte at p (the same p in all lanes), likewise: a scalar load has at least four bytes, those of the aligned word around it.
-__device__ __forceinline__ int scalar_byte(const unsigned char* p) {
-    return *(scalar_int)((uintptr_t)p & ~(uintptr_t)3) >> (8 * ((uintptr_t)p & 3)) & 255;
+// Byte i of the array p, likewise: a scalar load has at least four bytes, those of the aligned word around it (p is aligned).
+__device__ __forceinline__ int scalar_byte(const unsigned char* p, unsigned i) {
+    return ((scalar_int)p)[i >> 2] >> (8 * (i & 3)) & 255;
 }
-constexpr int kCounters = OT_PAGED_SYNC_BYTES / 4 - 1024;   // tickets, behind the kilo-word that ends with the status word
+constexpr int kTicketRows = 16;                              // up to so many rows of a block are joined by its last workgroup
 constexpr int kSplitBatch = 256;                             // sequences of a batch whose contexts are cut into ranges
 constexpr int kTile = 64;
 // reference of a row that has seen nothing: from it a masked score gives 0 and any score moves the reference
@@ -48,27 +48,37 @@ constexpr float kSlack = 8.f;
 // wavefront start (kernel-argument preload).
 struct Lead {
     const int32_t *prefix_len, *table;
-    int batch, units, max_pages, ps_log2, tiles_tree, ranges;      // ranges: jobs aimed at << 8 | fewest tiles of a range; 0: no ranges
+    int batch, units, max_pages, ps_log2, tiles_tree;
+    int target;                  // jobs aimed at; 0: every sequence in one piece
+    float apart;                 // what another range costs, in tiles
 };
 #define OT_LEAD_PARAMS const int32_t *l_prefix_len, const int32_t *l_table, const int l_batch, const int l_units, const int l_max_pages, \
-                       const int l_ps_log2, const int l_tiles_tree, const int l_ranges
-#define OT_LEAD Lead{l_prefix_len, l_table, l_batch, l_units, l_max_pages, l_ps_log2, l_tiles_tree, l_ranges}
+                       const int l_ps_log2, const int l_tiles_tree, const int l_target, const float l_apart
+#define OT_LEAD Lead{l_prefix_len, l_table, l_batch, l_units, l_max_pages, l_ps_log2, l_tiles_tree, l_target, l_apart}
 
 struct PagedArgs {
     const void *Q, *Kt, *Vt;
-    const unsigned char *kp, *vp;
     const unsigned char *k_exp, *v_exp;
     const uint64_t* mask;
     void* O;
     unsigned int* sync;
     float* part;                 // [job][rows of a block][D], then [job][rows][2] (reference, sum)
     float* part_ml;
+    int2* joins;                 // [sequence][unit] (first job, ranges), for the launch that joins; null: the last job joins
     int kv_heads, g, n, tree_keys, W, row_blocks, units;          // units = kv_heads * row_blocks
     int num_pages;
-    int slot_rows;               // rows of a partial
+    int block_rows, slot_rows;   // rows of a block, and of a partial
     float scale_log2;
-    long long qs[3], kts[3], vts[3], os[3], kps[3], vps[3];
+    long long qs[3], kts[3], vts[3], os[3];
+    unsigned k_page, v_page;     // page strides in units of 16 bytes
+    unsigned k_row, v_row;       // row strides in bytes
+    const unsigned char *kp, *vp;        // page 0
+    long long k_head, v_head;    // head strides in bytes
 };
+// Rows `row` .. of a page, as an address that is the same in all lanes
+__device__ __forceinline__ const unsigned char* row_of(const unsigned char* head, unsigned page, unsigned page_stride, unsigned row, unsigned row_stride) {
+    return head + ((u64)page * page_stride << 4) + row * row_stride;
+}
 
 __device__ __forceinline__ float xhalf_max(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -98,14 +108,15 @@ struct Job {
 };
 
 // Which range of which unit workgroup `wg` computes; the same in every lane of the workgroup.  Tiles per range are about the
-// fewest (at least `least`) with which all jobs together are no more than `target`: each sequence takes ceil(tiles / share)
-// ranges of equal length.  Lane j holds sequences j, j + 64, ...
+// fewest with which all jobs together are no more than `target`, and at least sqrt(T apart), T the tiles of the longest
+// sequence: S ranges take T / S tiles and S joins of `apart` tiles each, which is least there.  Each sequence takes
+// ceil(tiles / share) ranges of equal length.  Lane j holds sequences j, j + 64, ...
 __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int wg) {
     const int lane = threadIdx.x & 63, cap = a.max_pages << a.ps_log2;
     Job j;
     j.none = false;
     int raw;
-    if (!a.ranges) {
+    if (!a.target) {
         j.b = wg / a.units;
         j.unit = wg - j.b * a.units;
         j.splits = 1; j.split = 0; j.slot = 0;
@@ -113,7 +124,7 @@ __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int w
         raw = a.prefix_len[j.b];
     } else {
         constexpr int NL = kSplitBatch / 64;
-        const int target = a.ranges >> 8, least = a.ranges & 255;
+        const int target = a.target;
         const int u = wg / a.units;                      // which (sequence, range)
         j.unit = wg - u * a.units;
         int len[NL], T[NL], S[NL], most = 0;
@@ -130,7 +141,7 @@ __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int w
                 total += (float)wave_sum_i(T[i]);
                 most = max(most, wave_max_i(T[i]));
             }
-        int share = max(least, min(most, (int)ceilf(total * (float)a.units / (float)target)));
+        int share = max(1, min(most, (int)ceilf(fmaxf(total * (float)a.units / (float)target, sqrtf((float)most * a.apart)))));
         int jobs;
         while (true) {
             jobs = 0;
@@ -272,6 +283,15 @@ __device__ __forceinline__ void hide(f32x16& s, unsigned bits, int h) {
         if (!(bits >> (8 * (v >> 2) + (v & 3)) & 1)) s[v] = -INFINITY;
 }
 
+// A float4 of a partial, past the caches either way
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t part_buffer(float* part) { return __builtin_amdgcn_make_buffer_rsrc(part, 0, 0x7fffffff, 0x00020000); }
+constexpr int kDeviceScope = 16;             // cache policy of the buffer instructions: sc1
+__device__ __forceinline__ void put4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), b, (int)(at * 4), 0, kDeviceScope);
+}
+__device__ __forceinline__ f32x4 get4(__amdgpu_buffer_rsrc_t b, unsigned at) {
+    return __builtin_bit_cast(f32x4, (u32x4)__builtin_amdgcn_raw_buffer_load_b128(b, (int)(at * 4), 0, kDeviceScope));
+}
 __device__ __forceinline__ u64 pack2(float x, float y) { return (u64)__float_as_uint(x) | ((u64)__float_as_uint(y) << 32); }
 // Partials travel between workgroups on different XCDs: device-scope stores write through, device-scope loads read around
 // the caches, and every wavefront waits for its stores before the workgroup takes its ticket.
@@ -289,9 +309,48 @@ __device__ __forceinline__ unsigned short* out_row(const PagedArgs& a, int b, in
     return (unsigned short*)a.O + (long long)b * a.os[0] + (long long)(hk * a.g + head) * a.os[1] + (long long)node * a.os[2];
 }
 
-// After a workgroup has stored its partial: the last one of its row block adds all of them up, in the order of the ranges.
+// Four columns of a row: all its ranges added up, in their order.  Everything a chunk of ranges needs is requested before the
+// first of it is used.
+template <int D, int CHUNK>
+__device__ __forceinline__ f32x4 add_up(const PagedArgs& a, __amdgpu_buffer_rsrc_t part, int slot, int splits, int row, int col) {
+    float M = kNoRef, L = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < splits; s0 += CHUNK) {
+        float2 ml[CHUNK];
+        f32x4 x[CHUNK];
+#pragma unroll
+        for (int s = 0; s < CHUNK; ++s) {
+            const unsigned at = (unsigned)(slot + min(s0 + s, splits - 1) * a.units) * a.slot_rows + row;
+            ml[s] = get2(a.part_ml + at * 2);
+            x[s] = get4(part, at * D + col);
+        }
+        float to = M;
+#pragma unroll
+        for (int s = 0; s < CHUNK; ++s) to = fmaxf(to, ml[s].x);            // (a copy of the last range changes nothing)
+        const float f = __builtin_amdgcn_exp2f(M - to);
+        L *= f;
+        o *= f;
+#pragma unroll
+        for (int s = 0; s < CHUNK; ++s) {
+            const float w = s0 + s < splits ? __builtin_amdgcn_exp2f(ml[s].x - to) : 0.f;
+            L += ml[s].y * w;
+            o += x[s] * w;
+        }
+        M = to;
+    }
+    return o * inverse(L);
+}
+template <int D>
+__device__ __forceinline__ void store_joined(const PagedArgs& a, int b, int hk, int rho, int col, f32x4 y) {
+    *(uint2*)(out_row(a, b, hk, rho) + col) = uint2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+}
+
+// After a workgroup has stored its partial.  Few rows: the last workgroup of a row block joins them (ticket).  Many: that would
+// be one compute unit reading what all of them wrote (256 rows in 16 ranges: 50 us), so another launch joins, and the first
+// range says where the partials are.
 template <int D, int NT>
 __device__ __forceinline__ void join_splits(const PagedArgs& a, const Job& j, int hk, int row0, int rows, int* s_last) {
+    if (a.joins) return;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     unsigned int* const ticket = a.sync + 1024 + j.b * a.units + j.unit;
@@ -300,52 +359,25 @@ __device__ __forceinline__ void join_splits(const PagedArgs& a, const Job& j, in
     __syncthreads();
     if (!*s_last) return;
     if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // a thread adds up two columns of a row (few rows: every thread has some) or eight; all loads of a chunk of ranges are
-    // requested before the first is used, each is a trip to memory
-    auto join = [&](auto words_c, auto chunk_c) {
-        constexpr int WORDS = words_c, CHUNK = chunk_c, PER = D / (2 * WORDS);
-        for (int i = threadIdx.x; i < rows * PER; i += NT) {
-            const int row = i / PER, col = i % PER * 2 * WORDS;
-            float M = kNoRef, L = 0.f, o[2 * WORDS];
-#pragma unroll
-            for (int e = 0; e < 2 * WORDS; ++e) o[e] = 0.f;
-            for (int s0 = 0; s0 < j.splits; s0 += CHUNK) {
-                float2 ml[CHUNK], x[CHUNK][WORDS];
-#pragma unroll
-                for (int s = 0; s < CHUNK; ++s) {
-                    const size_t at = (size_t)(j.slot + min(s0 + s, j.splits - 1) * a.units) * a.slot_rows + row;
-                    ml[s] = get2(a.part_ml + at * 2);
-#pragma unroll
-                    for (int e = 0; e < WORDS; ++e) x[s][e] = get2(a.part + at * D + col + 2 * e);
-                }
-                float to = M;
-#pragma unroll
-                for (int s = 0; s < CHUNK; ++s) to = fmaxf(to, ml[s].x);            // (a copy of the last range changes nothing)
-                const float f = __builtin_amdgcn_exp2f(M - to);
-                L *= f;
-#pragma unroll
-                for (int e = 0; e < 2 * WORDS; ++e) o[e] *= f;
-#pragma unroll
-                for (int s = 0; s < CHUNK; ++s) {
-                    const float w = s0 + s < j.splits ? __builtin_amdgcn_exp2f(ml[s].x - to) : 0.f;
-                    L += ml[s].y * w;
-#pragma unroll
-                    for (int e = 0; e < WORDS; ++e) { o[2 * e] += x[s][e].x * w; o[2 * e + 1] += x[s][e].y * w; }
-                }
-                M = to;
-            }
-            const float inv = inverse(L);
-            unsigned short* const to = out_row(a, j.b, hk, row0 + row) + col;
-            if constexpr (WORDS == 1) *(unsigned*)to = pack_bf16(o[0] * inv, o[1] * inv);
-            else {
-#pragma unroll
-                for (int e = 0; e < 2 * WORDS; ++e) o[e] *= inv;
-                store8<OT_BF16>(to, 0, o);
-            }
-        }
-    };
-    if (rows * (D / 2) <= NT) join(std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
-    else join(std::integral_constant<int, 4>(), std::integral_constant<int, 8>());
+    const auto part = part_buffer(a.part);
+    for (int i = threadIdx.x; i < rows * (D / 4); i += NT) {
+        const int row = i / (D / 4), col = i % (D / 4) * 4;
+        store_joined<D>(a, j.b, hk, row0 + row, col, add_up<D, 16>(a, part, j.slot, j.splits, row, col));
+    }
+}
+__device__ __forceinline__ void note_splits(const PagedArgs& a, const Job& j) {
+    if (a.joins && j.split == 0 && threadIdx.x == 0) a.joins[j.b * a.units + j.unit] = int2{j.slot, j.splits};
+}
+
+// The launch that joins: a thread has four columns of a row
+template <int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
+    const int2 from = a.joins[blockIdx.y];
+    if (from.y == 1) return;
+    const int b = blockIdx.y / a.units, unit = blockIdx.y - b * a.units, hk = unit / a.row_blocks, rb = unit - hk * a.row_blocks;
+    const int row = blockIdx.x * (1024 / D) + threadIdx.x / (D / 4), col = threadIdx.x % (D / 4) * 4, rho = rb * a.block_rows + row;
+    if (row >= a.slot_rows || rho >= a.g * a.n) return;
+    store_joined<D>(a, b, hk, rho, col, add_up<D, 8>(a, part_buffer(a.part), from.x, from.y, row, col));
 }
 
 // ---------------------------------------------------------------------------
@@ -381,6 +413,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     int* const s_last = (int*)(s_sum + 4 * 32);
     const Job j = find_job(OT_LEAD, a.sync, blockIdx.x);
     if (j.none) return;
+    note_splits(a, j);
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const int qb = wave % QW, ks = wave / QW;
     const int hk = j.unit / a.row_blocks, rb = j.unit - hk * a.row_blocks;
@@ -444,7 +477,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const int blocks = (j.len + 31) / 32, ptiles = (j.len + kTile - 1) / kTile;
     const scalar_int table = (scalar_int)l_table + (long long)j.b * l_max_pages;
     const int ps = 1 << l_ps_log2, page_last = max(j.len - 1, 0) >> l_ps_log2;
-    bool bad = false;
+    unsigned bad = 0;              // rows of pages that are none
     struct Pages {
         int page[2];               // of the block's first and second sixteen rows
         unsigned seen;             // its rows that exist
@@ -457,45 +490,46 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         for (int e = 0; e < 2; ++e) r.page[e] = table[min((key0 + 16 * e) >> l_ps_log2, page_last)];
         return r;
     };
-    auto check = [&](int i, Pages& r) {
+    auto check = [&](Pages& r) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if ((unsigned)r.page[e] >= (unsigned)a.num_pages) {
-                if (32 * i + 16 * e < j.len) bad = true;
-                r.page[e] = 0;
-                r.seen &= e ? 0xffffu : 0xffff0000u;
-            }
+        for (int e = 0; e < 2; ++e) {
+            const bool there = (unsigned)r.page[e] < (unsigned)a.num_pages;
+            const unsigned rows = there ? 0u : 0xffffu << (16 * e);
+            bad |= r.seen & rows;
+            r.seen &= ~rows;
+            r.page[e] = there ? r.page[e] : 0;
+        }
     };
     constexpr int DIST = 1;         // blocks requested ahead
     u32x4 kr[DIST][KL], vr[DIST][KL];
     int ke[DIST][2], ve[DIST][2];                        // exponents of either half of the block
     // Every instruction asks for whole rows, and says that they are read once: 16 bytes of 32 rows each instead, as the matrix
     // operand wants them, or without the hint, 64 heads over 4 x 100000 keys take 172 us, not 156.
-    const unsigned k_lane = (unsigned)(lane / CPR) * (unsigned)(a.kps[2] * ESZ) + 16 * (lane % CPR);
-    const unsigned v_lane = (unsigned)(lane / CPR) * (unsigned)(a.vps[2] * ESZ) + 16 * (lane % CPR);
-    const unsigned char* const kh = a.kp + (long long)hk * a.kps[1] * ESZ;
-    const unsigned char* const vh = a.vp + (long long)hk * a.vps[1] * ESZ;
+    const unsigned k_lane = (unsigned)(lane / CPR) * a.k_row + 16 * (lane % CPR);
+    const unsigned v_lane = (unsigned)(lane / CPR) * a.v_row + 16 * (lane % CPR);
+    const unsigned char* const kh = a.kp + hk * a.k_head;
+    const unsigned char* const vh = a.vp + hk * a.v_head;
     auto load_k = [&](int i, const Pages& r, int at) {
         const unsigned char* b[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) b[e] = kh + ((long long)r.page[e] * a.kps[0] + (long long)((32 * i + 16 * e) & (ps - 1)) * a.kps[2]) * ESZ;
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if constexpr (KV8) ke[at][e] = scalar_byte(a.k_exp + ((long long)r.page[e] * a.kv_heads + hk));
+        for (int e = 0; e < 2; ++e) {
+            b[e] = row_of(kh, r.page[e], a.k_page, (32 * i + 16 * e) & (ps - 1), a.k_row);
+            if constexpr (KV8) ke[at][e] = scalar_byte(a.k_exp, (unsigned)r.page[e] * a.kv_heads + hk);
+        }
 #pragma unroll
         for (int n = 0; n < KL; ++n)                     // rows n RPL .. n RPL + RPL - 1 of the block
-            kr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + (long long)((n * RPL) & 15) * a.kps[2] * ESZ + k_lane));
+            kr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + ((n * RPL) & 15) * a.k_row + k_lane));
     };
     auto load_v = [&](int i, const Pages& r, int at) {
         const unsigned char* b[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            b[e] = vh + ((long long)r.page[e] * a.vps[0] + (long long)((32 * i + 16 * e) & (ps - 1)) * a.vps[2]) * ESZ;
-            if constexpr (KV8) ve[at][e] = scalar_byte(a.v_exp + ((long long)r.page[e] * a.kv_heads + hk));
+            b[e] = row_of(vh, r.page[e], a.v_page, (32 * i + 16 * e) & (ps - 1), a.v_row);
+            if constexpr (KV8) ve[at][e] = scalar_byte(a.v_exp, (unsigned)r.page[e] * a.kv_heads + hk);
         }
 #pragma unroll
         for (int n = 0; n < KL; ++n)
-            vr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + (long long)((n * RPL) & 15) * a.vps[2] * ESZ + v_lane));
+            vr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + ((n * RPL) & 15) * a.v_row + v_lane));
     };
     auto stage = [&](unsigned seen, int slot) {
         wave_fence();
@@ -548,7 +582,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             for (int d = 0; d < DIST; ++d) {
                 const int k = in_range(i + d * KS);
                 Pages p = pages_of(k);
-                check(k, p);
+                check(p);
                 load_v(k, p, d);
                 load_k(k, p, d);
                 seen[d] = p.seen;
@@ -559,7 +593,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 constexpr int slot = slot_c;
                 const int to = in_range(i + DIST * KS);
                 const Pages after = pages_of(in_range(i + DIST * KS + KS));
-                check(to, ahead);
+                check(ahead);
                 const unsigned now = seen[slot];
                 const int e0 = KV8 ? ke[slot][0] : 0, e1 = KV8 ? ke[slot][1] : 0;
                 stage(now, slot);
@@ -672,9 +706,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                 for (int e = 0; e < 8; ++e) y[e] *= inv;
                 store8<OT_BF16>(out_row(a, j.b, hk, row0 + q * 32 + row), 64 * part + col, y);
             } else {
-                const size_t at = (size_t)(j.slot + j.split * a.units) * a.slot_rows + q * 32 + row;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) put2(a.part + at * D + 64 * part + col + 2 * e, y[2 * e], y[2 * e + 1]);
+                const unsigned at = (unsigned)(j.slot + j.split * a.units) * a.slot_rows + q * 32 + row;
+                put4(part_buffer(a.part), at * D + 64 * part + col, f32x4{y[0], y[1], y[2], y[3]});
+                put4(part_buffer(a.part), at * D + 64 * part + col + 4, f32x4{y[4], y[5], y[6], y[7]});
                 if (part == 0 && col == 0) put2(a.part_ml + at * 2, M[q], L[q]);
             }
         }
@@ -704,6 +738,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     auto v_buf = [&](int i) { return s_kv + (2 + i) * TILE; };                   // two of V, three if the wavefronts take turns
     const Job j = find_job(OT_LEAD, a.sync, blockIdx.x);
     if (j.none) return;
+    note_splits(a, j);
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, h = lane >> 5;
     const int hk = j.unit / a.row_blocks, rb = j.unit - hk * a.row_blocks;
     const int rows_all = a.g * a.n, row0 = rb * 32 * NW, rows = min(32 * NW, rows_all - row0);
@@ -730,7 +765,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int ptiles = (j.len + kTile - 1) / kTile;
     const scalar_int table = (scalar_int)l_table + (long long)j.b * l_max_pages;
     const int ps = 1 << l_ps_log2, page_last = max(j.len - 1, 0) >> l_ps_log2;
-    bool bad = false;
+    u64 bad = 0;                                         // rows of pages that are none
     const int e_wave = wave * (64 / CPM);                // first row of this wavefront's first request; the others NT / CPM rows on
 
     auto put_k = [&](unsigned short* sk, int row, int piece, const u32x4& w) { *(u32x4*)(sk + row * D + ((piece ^ (row & (CPR - 1))) << 3)) = w; };
@@ -794,29 +829,30 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         u32x4 kr[CH], vr[CH];
         int ke[CH], ve[CH];
         u64 next = 0;                      // rows of the tile in registers that exist
-        const unsigned k_lane = (unsigned)(lane / CPM) * (unsigned)(a.kps[2] * ESZ) + 16 * (lane % CPM);
-        const unsigned v_lane = (unsigned)(lane / CPM) * (unsigned)(a.vps[2] * ESZ) + 16 * (lane % CPM);
-        auto load = [&](int t, Pages r) {        // past the last tile: that one again (a load under a condition makes waits longer)
+        const unsigned k_lane = (unsigned)(lane / CPM) * a.k_row + 16 * (lane % CPM);
+        const unsigned v_lane = (unsigned)(lane / CPM) * a.v_row + 16 * (lane % CPM);
+        const unsigned char* const kh = a.kp + hk * a.k_head;
+        const unsigned char* const vh = a.vp + hk * a.v_head;
+        auto load = [&](int t, Pages r) {                // past the last tile: that one again (a load under a condition makes waits longer)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if ((unsigned)r.page[e] >= (unsigned)a.num_pages) {
-                    if (t * kTile + 16 * e < j.len) bad = true;
-                    r.page[e] = 0;
-                    r.seen &= ~(0xffffull << (16 * e));
-                }
+            for (int e = 0; e < 4; ++e) {
+                const bool there = (unsigned)r.page[e] < (unsigned)a.num_pages;
+                const u64 rows = there ? 0ull : 0xffffull << (16 * e);
+                bad |= r.seen & rows;
+                r.seen &= ~rows;
+                r.page[e] = there ? r.page[e] : 0;
+            }
             next = r.seen;
 #pragma unroll
             for (int n = 0; n < CH; ++n) {
                 const int first = e_wave + n * (NT / CPM), e = first >> 4;       // rows first .. first + 64 / CPM - 1
-                const int page = e == 0 ? r.page[0] : e == 1 ? r.page[1] : e == 2 ? r.page[2] : r.page[3];
-                const int row = (t * kTile + first) & (ps - 1);
-                const unsigned char* const kb = a.kp + ((long long)page * a.kps[0] + (long long)hk * a.kps[1] + (long long)row * a.kps[2]) * ESZ;
-                const unsigned char* const vb = a.vp + ((long long)page * a.vps[0] + (long long)hk * a.vps[1] + (long long)row * a.vps[2]) * ESZ;
-                kr[n] = *(const u32x4*)(kb + k_lane);
-                vr[n] = *(const u32x4*)(vb + v_lane);
+                const unsigned page = e == 0 ? r.page[0] : e == 1 ? r.page[1] : e == 2 ? r.page[2] : r.page[3];
+                const unsigned row = (t * kTile + first) & (ps - 1);
+                kr[n] = *(const u32x4*)(row_of(kh, page, a.k_page, row, a.k_row) + k_lane);
+                vr[n] = *(const u32x4*)(row_of(vh, page, a.v_page, row, a.v_row) + v_lane);
                 if constexpr (KV8) {
-                    ke[n] = scalar_byte(a.k_exp + ((long long)page * a.kv_heads + hk));
-                    ve[n] = scalar_byte(a.v_exp + ((long long)page * a.kv_heads + hk));
+                    ke[n] = scalar_byte(a.k_exp, page * a.kv_heads + hk);
+                    ve[n] = scalar_byte(a.v_exp, page * a.kv_heads + hk);
                 }
             }
         };
@@ -873,7 +909,9 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
                 weights(visible);
                 __syncthreads();
                 if (++t >= tp1) break;
+                __builtin_amdgcn_s_setprio(1);           // (the matrix side is issued first: 582 -> 570 us)
                 values_and_scores(v_buf(va), k_buf((t - j.t0) & 1));
+                __builtin_amdgcn_s_setprio(0);
                 va = va == 2 ? 0 : va + 1;
             }
             if (!second) __syncthreads();
@@ -952,11 +990,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
         return;
     }
     if (row < rows) {
-        const size_t at = (size_t)(j.slot + j.split * a.units) * a.slot_rows + row;
+        const unsigned at = (unsigned)(j.slot + j.split * a.units) * a.slot_rows + row;
 #pragma unroll
         for (int d = 0; d < DB; ++d)
 #pragma unroll
-            for (int v = 0; v < 8; ++v) put2(a.part + at * D + 32 * d + 8 * (v >> 1) + 4 * h + 2 * (v & 1), o[d][2 * v], o[d][2 * v + 1]);
+            for (int v = 0; v < 4; ++v)
+                put4(part_buffer(a.part), at * D + 32 * d + 8 * v + 4 * h, f32x4{o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]});
         if (h == 0) put2(a.part_ml + at * 2, ref, L);
     }
     __shared__ int s_last;
@@ -966,8 +1005,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
 __global__ __launch_bounds__(256) void clear_words_kernel(unsigned int* w) { w[blockIdx.x * 256 + threadIdx.x] = 0; }
 
 struct PagedPlan {
-    int rows, row_blocks, units, split, target, least, grid, slot_rows;
-    size_t bytes;
+    int rows, row_blocks, units, target, grid, slot_rows;
+    bool late;                // another launch joins
+    float apart;
+    size_t part_bytes, ml_bytes, bytes;
 };
 
 PagedPlan plan_paged(const ot_paged_attn_params& p, const ot_paged_cache& c) {
@@ -977,15 +1018,20 @@ PagedPlan plan_paged(const ot_paged_attn_params& p, const ot_paged_cache& c) {
     pl.rows = R <= 32 ? 32 : R <= 64 ? 64 : R <= 128 || (c.head_dim == 64 && c.dtype == OT_E4M3) ? 128 : 256;
     pl.row_blocks = (R + pl.rows - 1) / pl.rows;
     pl.units = c.kv_heads * pl.row_blocks;
-    const long long all = (long long)p.batch * pl.units;
-    pl.split = p.batch <= kSplitBatch && all <= kCounters;
-    pl.target = pl.rows <= 128 ? 512 : 256;
-    pl.least = pl.rows <= 32 ? 2 : 4;
-    const long long tiles = ((long long)c.max_pages * c.page_size + kTile - 1) / kTile + (p.tree_keys + kTile - 1) / kTile;
-    const long long most = std::max<long long>(all, pl.target);
-    pl.grid = (int)(pl.split ? std::min(most, all * ((tiles + pl.least - 1) / pl.least)) : all);
     pl.slot_rows = std::min(R, pl.rows);
-    pl.bytes = OT_PAGED_SYNC_BYTES + (pl.split ? (size_t)pl.grid * pl.slot_rows * (c.head_dim + 2) * 4 : 0);
+    const long long all = (long long)p.batch * pl.units;
+    const int resident = pl.rows <= 128 ? 512 : 256;           // workgroups that the card holds
+    pl.target = p.batch <= kSplitBatch && all < resident ? resident : 0;
+    pl.grid = pl.target ? pl.target : (int)all;
+    pl.late = pl.target && pl.slot_rows > kTicketRows;
+    // A range more costs a partial written and read by every unit, at 4 TB/s, or a trip to memory for a chunk of sixteen; a
+    // tile of 64 keys takes (us, head_dim 128) 0.35 for up to 64 rows, 1.2 for 128, 2.2 for 256.
+    const float tile = (pl.rows <= 64 ? 0.35f : pl.rows == 128 ? 1.2f : 2.2f) * (float)c.head_dim / 128.f;
+    pl.apart = (pl.late ? (float)all * (float)pl.slot_rows * (float)c.head_dim * 8.f / 4e6f + 0.02f : 0.13f) / tile;
+    const size_t jobs = pl.target ? (size_t)pl.grid : 0;
+    pl.part_bytes = jobs * pl.slot_rows * c.head_dim * 4;
+    pl.ml_bytes = jobs * pl.slot_rows * 8;
+    pl.bytes = OT_PAGED_SYNC_BYTES + pl.part_bytes + pl.ml_bytes + (pl.late ? (size_t)all * sizeof(int2) : 0);
     return pl;
 }
 
@@ -1006,7 +1052,7 @@ int validate_paged(const ot_paged_attn_params* p, const ot_paged_cache* c, bool 
 
 template <int D, bool KV8>
 int launch_paged(const Lead& l, const PagedArgs& a, const PagedPlan& pl, hipStream_t s) {
-#define OT_LEAD_ARGS l.prefix_len, l.table, l.batch, l.units, l.max_pages, l.ps_log2, l.tiles_tree, l.ranges
+#define OT_LEAD_ARGS l.prefix_len, l.table, l.batch, l.units, l.max_pages, l.ps_log2, l.tiles_tree, l.target, l.apart
     constexpr size_t tile = (size_t)kTile * D * 2;
     if (pl.rows == 32) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 1>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
     else if (pl.rows == 64) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 2>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
@@ -1018,6 +1064,9 @@ int launch_paged(const Lead& l, const PagedArgs& a, const PagedPlan& pl, hipStre
         hipLaunchKernelGGL((paged_tiles_kernel<D, KV8, 8>), dim3(pl.grid), dim3(512), 5 * tile, s, OT_LEAD_ARGS, a);
     }
 #undef OT_LEAD_ARGS
+    OT_HIP_CHECK(hipGetLastError());
+    if (!pl.late) return OT_OK;
+    hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)((pl.slot_rows + 1024 / D - 1) / (1024 / D)), (unsigned)(l.batch * l.units)), dim3(256), 0, s, a);
     OT_HIP_CHECK(hipGetLastError());
     return OT_OK;
 }
@@ -1057,18 +1106,22 @@ int ot_tree_verify_attention_paged(const ot_paged_attn_params* p, const ot_paged
     a.k_exp = cache->k_exp; a.v_exp = cache->v_exp; a.mask = mask;
     a.sync = (unsigned int*)workspace;
     a.part = (float*)((char*)workspace + OT_PAGED_SYNC_BYTES);
-    a.part_ml = a.part + (size_t)pl.grid * pl.slot_rows * cache->head_dim;
+    a.part_ml = a.part + pl.part_bytes / 4;
+    a.joins = pl.late ? (int2*)((char*)a.part_ml + pl.ml_bytes) : nullptr;
     a.kv_heads = cache->kv_heads; a.g = p->q_heads / cache->kv_heads; a.n = p->n;
     a.tree_keys = p->tree_keys; a.W = OT_MASK_WORDS(p->tree_keys);
     a.row_blocks = pl.row_blocks; a.units = pl.units;
-    a.num_pages = cache->num_pages; a.slot_rows = pl.slot_rows;
+    a.num_pages = cache->num_pages; a.block_rows = pl.rows; a.slot_rows = pl.slot_rows;
     const Lead lead{prefix_len, cache->page_table, p->batch, pl.units, cache->max_pages, log2_of(cache->page_size),
-                    (p->tree_keys + kTile - 1) / kTile, pl.split ? pl.target << 8 | pl.least : 0};
+                    (p->tree_keys + kTile - 1) / kTile, pl.target, pl.apart};
     a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * kLog2e;
     for (int i = 0; i < 3; ++i) {
         a.qs[i] = p->q_strides[i]; a.kts[i] = p->kt_strides[i]; a.vts[i] = p->vt_strides[i]; a.os[i] = p->o_strides[i];
-        a.kps[i] = cache->k_strides[i]; a.vps[i] = cache->v_strides[i];
     }
+    const long long esz = cache->dtype == OT_E4M3 ? 1 : 2;
+    a.k_page = (unsigned)(cache->k_strides[0] * esz / 16); a.v_page = (unsigned)(cache->v_strides[0] * esz / 16);
+    a.k_row = (unsigned)(cache->k_strides[2] * esz); a.v_row = (unsigned)(cache->v_strides[2] * esz);
+    a.k_head = cache->k_strides[1] * esz; a.v_head = cache->v_strides[1] * esz;
     hipStream_t s = (hipStream_t)hip_stream;
     if (cache->dtype == OT_E4M3) return cache->head_dim == 128 ? launch_paged<128, true>(lead, a, pl, s) : launch_paged<64, true>(lead, a, pl, s);
     return cache->head_dim == 128 ? launch_paged<128, false>(lead, a, pl, s) : launch_paged<64, false>(lead, a, pl, s);
