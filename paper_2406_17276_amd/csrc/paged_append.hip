@@ -40,25 +40,31 @@ __device__ __forceinline__ int exponent_for(float top) {
 }
 __device__ __forceinline__ float power_of(int e) { return __uint_as_float((unsigned)e << 23); }   // 2^(e - 127), e in 1..254
 
+// max(a, |b|, |c|); a NaN loses
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 // |x| of finite x, 0 otherwise
 __device__ __forceinline__ float finite_abs(float x) {
     const unsigned u = __float_as_uint(x) & 0x7fffffffu;
     return u < 0x7f800000u ? __uint_as_float(u) : 0.f;
 }
-// E4M3 bytes of x and y, to nearest even; magnitudes over 448 (only infinities are, here) become 448, NaNs stay
-__device__ __forceinline__ float saturate(float x) { return x > 448.f ? 448.f : (x < -448.f ? -448.f : x); }
+// E4M3 bytes, to nearest even; NaNs stay NaNs
 __device__ __forceinline__ unsigned pack_e4m3(float x, float y, float z, float w) {
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(saturate(x), saturate(y), 0, false);
-    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(saturate(z), saturate(w), r, true);
+    int r = __builtin_amdgcn_cvt_pk_fp8_f32(x, y, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(z, w, r, true);
 }
+__device__ __forceinline__ float saturate(float x) { return x > 448.f ? 448.f : (x < -448.f ? -448.f : x); }
 
-template <int DT, bool KV8, int D, int NT>
+template <int DT, bool KV8, int D, int NT, int PASSES>
 __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a) {
     constexpr int LPR = D / 16;                // lanes per row
     constexpr int HALF = NT / 2;               // threads of the keys, and of the values
     constexpr int RPP = HALF / LPR;            // rows per pass
-    constexpr int PASSES = 4;                  // a page has at most PASSES * RPP rows (host)
-    extern __shared__ float2 s_cs[];           // [page rows][R / 2]
+    // a page has at most PASSES * RPP rows (host)
+    extern __shared__ __attribute__((aligned(16))) float2 s_cs[];               // [page rows][R / 2]
     __shared__ float s_top[NT / 64];
     const int tid = threadIdx.x, wave = tid >> 6;
     const bool val = tid >= HALF;
@@ -100,7 +106,7 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
         for (int i = tid; i < (row1 - row0) * half; i += NT) {
             const int r = i / half, j = i - r * half;
             const long long pos = ((long long)page_slot << a.ps_log2) + row0 + r + a.shift;
-            s_cs[(row0 + r) * half + j] = cos_sin((double)pos * a.rot.inv_freq[j]);
+            s_cs[(row0 + r) * half + angle_at(j, half / 8)] = cos_sin((double)pos * a.rot.inv_freq[j]);
         }
         __syncthreads();
     }
@@ -139,25 +145,42 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
             const int r = r_first + p * RPP;
             if (turns && r >= row0 && r < row1) {
                 float2 cs[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) cs[e] = s_cs[r * half + 8 * t + e];
+                read_angles(s_cs + r * half, t, half / 8, cs);
                 turn(xa[p], xb[p], cs, a.rot.interleaved);
             }
             if constexpr (KV8) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_abs(xa[p][e]), finite_abs(xb[p][e])));
+                for (int e = 0; e < 8; ++e) top = max3_abs(top, xa[p][e], xb[p][e]);
             }
         }
         unsigned char* const row_base = dst + ((long long)page * ds[0] + (long long)h * ds[1]) * ESZ;
         float f = 1.f;
+        bool infinite = false;
         if constexpr (KV8) {
-            top = wave_max(top);
-            __syncthreads();                                       // (s_top of the head before has been read)
-            if ((tid & 63) == 0) s_top[wave] = top;
-            __syncthreads();
-            constexpr int HW = NT / 128;                           // wavefronts of a half
+            // over the half's wavefronts, and over all
+            constexpr int HW = NT / 128;
+            auto over = [&](float v, float& all) {
+                v = wave_max_f(v);
+                __syncthreads();                                   // (what was in s_top has been read)
+                if ((tid & 63) == 0) s_top[wave] = v;
+                __syncthreads();
+                float k = 0.f, w = 0.f;
 #pragma unroll
-            for (int w = 0; w < HW; ++w) top = fmaxf(top, s_top[(val ? HW : 0) + w]);
+                for (int i = 0; i < HW; ++i) { k = fmaxf(k, s_top[i]); w = fmaxf(w, s_top[HW + i]); }
+                all = fmaxf(k, w);
+                return val ? w : k;
+            };
+            float all;
+            top = over(top, all);
+            infinite = all > 3.402823466e38f;
+            if (infinite) {                                        // the exponent is that of the finite values
+                top = 0.f;
+#pragma unroll
+                for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fmaxf(finite_abs(xa[p][e]), finite_abs(xb[p][e])));
+                top = over(top, all);
+            }
             unsigned char* const exp_at = (val ? a.v_exp : a.k_exp) + (long long)page * a.heads + h;
             int e = exponent_for(top);
             if (row0 > 0) {
@@ -179,7 +202,14 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
                 e = max(e, e_old);
             }
             f = power_of(254 - e);
-            __syncthreads();                                       // every lane has read the old exponent
+            if (infinite) {
+#pragma unroll
+                for (int p = 0; p < PASSES; ++p)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) { xa[p][i] = saturate(xa[p][i] * f); xb[p][i] = saturate(xb[p][i] * f); }
+                f = 1.f;
+            }
+            if (row0 > 0) __syncthreads();                         // every lane has read the old exponent
             if (ht == 0) *exp_at = (unsigned char)e;
         }
 #pragma unroll
@@ -219,23 +249,22 @@ bool overlap(const void* x, size_t nx, const void* y, size_t ny) {
     return x && y && (uintptr_t)x < (uintptr_t)y + ny && (uintptr_t)y < (uintptr_t)x + nx;
 }
 
-template <int DT, bool KV8, int D, int NT>
+template <int DT, bool KV8, int D, int NT, int PASSES>
 int launch(const AppendArgs& a, const dim3& grid, size_t lds, hipStream_t s) {
     if (lds > 64 * 1024)
-        OT_HIP_CHECK(hipFuncSetAttribute((const void*)kv_append_paged_kernel<DT, KV8, D, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((kv_append_paged_kernel<DT, KV8, D, NT>), grid, dim3(NT), lds, s, a);
+        OT_HIP_CHECK(hipFuncSetAttribute((const void*)kv_append_paged_kernel<DT, KV8, D, NT, PASSES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((kv_append_paged_kernel<DT, KV8, D, NT, PASSES>), grid, dim3(NT), lds, s, a);
     return OT_OK;
 }
+// Threads by the page's elements: two passes, which leaves room for 16 wavefronts and more on a compute unit (four passes of half
+// the threads: 12).
 template <int DT, bool KV8>
 int launch_for(const AppendArgs& a, int D, const dim3& grid, size_t lds, hipStream_t s) {
-    const int ps = 1 << a.ps_log2;
-    if (D == 128) {
-        if (ps <= 64) return launch<DT, KV8, 128, 256>(a, grid, lds, s);
-        if (ps == 128) return launch<DT, KV8, 128, 512>(a, grid, lds, s);
-        return launch<DT, KV8, 128, 1024>(a, grid, lds, s);
-    }
-    if (ps <= 128) return launch<DT, KV8, 64, 256>(a, grid, lds, s);
-    return launch<DT, KV8, 64, 512>(a, grid, lds, s);
+    const int elements = D << a.ps_log2;
+    if (elements <= 4096) return D == 128 ? launch<DT, KV8, 128, 256, 2>(a, grid, lds, s) : launch<DT, KV8, 64, 256, 2>(a, grid, lds, s);
+    if (elements <= 8192) return D == 128 ? launch<DT, KV8, 128, 512, 2>(a, grid, lds, s) : launch<DT, KV8, 64, 512, 2>(a, grid, lds, s);
+    if (elements <= 16384) return D == 128 ? launch<DT, KV8, 128, 1024, 2>(a, grid, lds, s) : launch<DT, KV8, 64, 1024, 2>(a, grid, lds, s);
+    return launch<DT, KV8, 128, 1024, 4>(a, grid, lds, s);
 }
 
 }  // namespace

@@ -36,7 +36,7 @@ template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void qk_rope_kernel(const QkKArgs a) {
     constexpr int LPR = D / 16;                       // lanes per row
     constexpr int RPP = kThreads / LPR;               // rows per pass
-    __shared__ float2 s_cs[kMaxTokens][D / 2];
+    __shared__ __attribute__((aligned(16))) float2 s_cs[kMaxTokens][D / 2];
     const int tid = threadIdx.x, t = tid % LPR;
     const int tok0 = a.base + (int)blockIdx.x * a.tokens, ntok = min(a.tokens, a.all_tokens - tok0);
     const int half = a.rot.dim / 2;
@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(const QkKArgs a) {
         const int k = i / half, j = i - k * half, tok = tok0 + k, b = tok / a.n;
         const int step = a.offset ? a.offset[tok] : tok - b * a.n;
         const long long pos = (long long)a.first[b] + step + a.shift;
-        s_cs[k][j] = cos_sin((double)pos * a.rot.inv_freq[j]);
+        s_cs[k][angle_at(j, a.rot.dim / 16)] = cos_sin((double)pos * a.rot.inv_freq[j]);
     }
     __syncthreads();
     const int ca = run_a(a.rot, t), cb = run_b(a.rot, t);
@@ -77,8 +77,7 @@ __global__ __launch_bounds__(kThreads) void qk_rope_kernel(const QkKArgs a) {
         }
         if (turns) {
             float2 cs[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) cs[e] = s_cs[k][8 * t + e];
+            read_angles(s_cs[k], t, a.rot.dim / 16, cs);
             turn(xa, xb, cs, a.rot.interleaved);
         }
         store8<DT>(q ? a.Qo : a.Ko, out + ca, xa);

@@ -73,6 +73,18 @@ __device__ __forceinline__ void turn(float (&a)[8], float (&b)[8], const float2 
     }
 }
 
+// Where the cosine and sine of angle j of a row sit among the row's R/2 in LDS: the lanes of a row read 16 bytes, two angles,
+// side by side.  lanes: R / 16, the lanes that turn.
+__device__ __forceinline__ int angle_at(int j, int lanes) { return ((j >> 1 & 3) * lanes + (j >> 3)) * 2 + (j & 1); }
+__device__ __forceinline__ void read_angles(const float2* row, int t, int lanes, float2 (&cs)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const f32x4 w = *(const f32x4*)(row + (e * lanes + t) * 2);
+        cs[2 * e] = float2{w[0], w[1]};
+        cs[2 * e + 1] = float2{w[2], w[3]};
+    }
+}
+
 // Eight consecutive values of a row in memory <-> fp32
 template <int DT> __device__ __forceinline__ void load8(const void* p, long long at, float (&x)[8]) {
     if constexpr (DT == OT_BF16) {
