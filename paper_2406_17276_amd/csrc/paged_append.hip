@@ -58,17 +58,17 @@ __device__ __forceinline__ unsigned pack_e4m3(float x, float y, float z, float w
 }
 __device__ __forceinline__ float saturate(float x) { return x > 448.f ? 448.f : (x < -448.f ? -448.f : x); }
 
-template <int DT, bool KV8, int D, int NT, int PASSES>
+template <int DT, bool KV8, int D, int NT, bool TOGETHER>
 __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a) {
     constexpr int LPR = D / 16;                // lanes per row
-    constexpr int HALF = NT / 2;               // threads of the keys, and of the values
+    constexpr int PASSES = 2;
+    constexpr int HALF = TOGETHER ? NT / 2 : NT;       // threads of the keys, and of the values
     constexpr int RPP = HALF / LPR;            // rows per pass
     // a page has at most PASSES * RPP rows (host)
     extern __shared__ __attribute__((aligned(16))) float2 s_cs[];               // [page rows][R / 2]
     __shared__ float s_top[NT / 64];
     const int tid = threadIdx.x, wave = tid >> 6;
-    const bool val = tid >= HALF;
-    const int ht = val ? tid - HALF : tid, t = ht % LPR, r_first = ht / LPR;
+    const int ht = tid % HALF, t = ht % LPR, r_first = ht / LPR;
     const int b = a.base + blockIdx.z;
     const int ps = 1 << a.ps_log2, cap = a.max_pages << a.ps_log2;
     const int len = min(max(a.cache_len[b], 0), cap);
@@ -110,6 +110,10 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
         }
         __syncthreads();
     }
+    const int h1 = min(a.heads, (int)(blockIdx.y + 1) * a.share);
+    // keys and values side by side, or one after the other
+    for (int turn_of = 0; turn_of < (TOGETHER ? 1 : 2); ++turn_of) {
+    const bool val = TOGETHER ? tid >= HALF : turn_of == 1;
     const bool turns = !val && 16 * t < a.rot.dim;
     const int ca = val ? 16 * t : run_a(a.rot, t), cb = val ? 16 * t + 8 : run_b(a.rot, t);
     const long long ss[3] = {val ? a.vs[0] : a.ks[0], val ? a.vs[1] : a.ks[1], val ? a.vs[2] : a.ks[2]};
@@ -127,7 +131,6 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
             if ((unsigned)i < (unsigned)a.n) from[p] = (long long)b * ss[0] + (long long)i * ss[2];
         }
     }
-    const int h1 = min(a.heads, (int)(blockIdx.y + 1) * a.share);
     for (int h = blockIdx.y * a.share; h < h1; ++h) {
         float xa[PASSES][8], xb[PASSES][8];
         float top = 0.f;
@@ -157,8 +160,8 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
         float f = 1.f;
         bool infinite = false;
         if constexpr (KV8) {
-            // over the half's wavefronts, and over all
-            constexpr int HW = NT / 128;
+            // over the wavefronts of the keys or the values, and over all
+            constexpr int HW = TOGETHER ? NT / 128 : NT / 64;
             auto over = [&](float v, float& all) {
                 v = wave_max_f(v);
                 __syncthreads();                                   // (what was in s_top has been read)
@@ -166,9 +169,9 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
                 __syncthreads();
                 float k = 0.f, w = 0.f;
 #pragma unroll
-                for (int i = 0; i < HW; ++i) { k = fmaxf(k, s_top[i]); w = fmaxf(w, s_top[HW + i]); }
+                for (int i = 0; i < HW; ++i) { k = fmaxf(k, s_top[i]); if (TOGETHER) w = fmaxf(w, s_top[HW + i]); }
                 all = fmaxf(k, w);
-                return val ? w : k;
+                return TOGETHER && val ? w : k;
             };
             float all;
             top = over(top, all);
@@ -227,6 +230,7 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
             }
         }
     }
+    }
 }
 
 int validate_append(const ot_append_params* p, const ot_paged_cache* c) {
@@ -249,22 +253,22 @@ bool overlap(const void* x, size_t nx, const void* y, size_t ny) {
     return x && y && (uintptr_t)x < (uintptr_t)y + ny && (uintptr_t)y < (uintptr_t)x + nx;
 }
 
-template <int DT, bool KV8, int D, int NT, int PASSES>
+template <int DT, bool KV8, int D, int NT, bool TOGETHER>
 int launch(const AppendArgs& a, const dim3& grid, size_t lds, hipStream_t s) {
     if (lds > 64 * 1024)
-        OT_HIP_CHECK(hipFuncSetAttribute((const void*)kv_append_paged_kernel<DT, KV8, D, NT, PASSES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
-    hipLaunchKernelGGL((kv_append_paged_kernel<DT, KV8, D, NT, PASSES>), grid, dim3(NT), lds, s, a);
+        OT_HIP_CHECK(hipFuncSetAttribute((const void*)kv_append_paged_kernel<DT, KV8, D, NT, TOGETHER>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    hipLaunchKernelGGL((kv_append_paged_kernel<DT, KV8, D, NT, TOGETHER>), grid, dim3(NT), lds, s, a);
     return OT_OK;
 }
-// Threads by the page's elements: two passes, which leaves room for 16 wavefronts and more on a compute unit (four passes of half
-// the threads: 12).
+// Threads by the page's elements: two passes over its rows, which leaves room for 16 wavefronts and more on a compute unit (four
+// passes of half the threads: 12; 8 prompts of 8192 rows 107 us, not 83).
 template <int DT, bool KV8>
 int launch_for(const AppendArgs& a, int D, const dim3& grid, size_t lds, hipStream_t s) {
     const int elements = D << a.ps_log2;
-    if (elements <= 4096) return D == 128 ? launch<DT, KV8, 128, 256, 2>(a, grid, lds, s) : launch<DT, KV8, 64, 256, 2>(a, grid, lds, s);
-    if (elements <= 8192) return D == 128 ? launch<DT, KV8, 128, 512, 2>(a, grid, lds, s) : launch<DT, KV8, 64, 512, 2>(a, grid, lds, s);
-    if (elements <= 16384) return D == 128 ? launch<DT, KV8, 128, 1024, 2>(a, grid, lds, s) : launch<DT, KV8, 64, 1024, 2>(a, grid, lds, s);
-    return launch<DT, KV8, 128, 1024, 4>(a, grid, lds, s);
+    if (elements <= 4096) return D == 128 ? launch<DT, KV8, 128, 256, true>(a, grid, lds, s) : launch<DT, KV8, 64, 256, true>(a, grid, lds, s);
+    if (elements <= 8192) return D == 128 ? launch<DT, KV8, 128, 512, true>(a, grid, lds, s) : launch<DT, KV8, 64, 512, true>(a, grid, lds, s);
+    if (elements <= 16384) return D == 128 ? launch<DT, KV8, 128, 1024, true>(a, grid, lds, s) : launch<DT, KV8, 64, 1024, true>(a, grid, lds, s);
+    return launch<DT, KV8, 128, 1024, false>(a, grid, lds, s);
 }
 
 }  // namespace
