@@ -1025,8 +1025,8 @@ PagedPlan plan_paged(const ot_paged_attn_params& p, const ot_paged_cache& c) {
     pl.grid = pl.target ? pl.target : (int)all;
     pl.late = pl.target && pl.slot_rows > kTicketRows;
     // A range more costs a partial written and read by every unit, at 4 TB/s, or a trip to memory for a chunk of sixteen; a
-    // tile of 64 keys takes (us, head_dim 128) 0.35 for up to 64 rows, 1.2 for 128, 2.2 for 256.
-    const float tile = (pl.rows <= 64 ? 0.35f : pl.rows == 128 ? 1.2f : 2.2f) * (float)c.head_dim / 128.f;
+    // tile of 64 keys takes (us, head_dim 128) 0.7 for up to 64 rows, 1.2 for 128, 2.2 for 256.
+    const float tile = (pl.rows <= 64 ? 0.7f : pl.rows == 128 ? 1.2f : 2.2f) * (float)c.head_dim / 128.f;
     pl.apart = (pl.late ? (float)all * (float)pl.slot_rows * (float)c.head_dim * 8.f / 4e6f + 0.02f : 0.13f) / tile;
     const size_t jobs = pl.target ? (size_t)pl.grid : 0;
     pl.part_bytes = jobs * pl.slot_rows * c.head_dim * 4;

@@ -133,7 +133,7 @@ int ot_qk_norm_rope(const ot_qk_params* p, const void* Q, const void* K, const v
     a.shift = p->shift; a.eps = p->eps;
     for (int i = 0; i < 3; ++i) { a.qs[i] = p->q_strides[i]; a.ks[i] = p->k_strides[i]; a.qos[i] = p->qo_strides[i]; a.kos[i] = p->ko_strides[i]; }
     const int rpp = kThreads * 16 / p->head_dim;
-    a.tokens = std::min(kMaxTokens, std::max(1, 4 * rpp / a.heads));
+    a.tokens = std::min(kMaxTokens, std::max(1, 2 * rpp / a.heads));
     a.share = a.heads;
     if ((a.all_tokens + a.tokens - 1) / a.tokens < 512) {      // few tokens: a token each, heads over several workgroups
         a.tokens = 1;
