@@ -481,8 +481,9 @@ def paged_params(Q, cache: PagedCache, K_tree=None, V_tree=None, softmax_scale: 
     p = PagedAttnParams(Q.shape[0], Q.shape[1], Q.shape[2], 0 if K_tree is None else K_tree.shape[2], float(softmax_scale), st(Q),
                         st(K_tree), st(V_tree), st(Q))
     ptr = lambda t: None if t is None else t.data_ptr()
+    import torch
     P, H, ps, D = cache.k.shape
-    c = PagedCacheParams(P, ps, H, D, OT_BF16 if cache.k_exp is None else OT_E4M3, cache.table.shape[1], st(cache.k), st(cache.v),
+    c = PagedCacheParams(P, ps, H, D, OT_BF16 if cache.k.dtype == torch.bfloat16 else OT_E4M3, cache.table.shape[1], st(cache.k), st(cache.v),
                          ptr(cache.k), ptr(cache.v), ptr(cache.k_exp), ptr(cache.v_exp), ptr(cache.table))
     return p, c
 

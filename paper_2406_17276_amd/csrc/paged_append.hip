@@ -5,10 +5,13 @@
 //
 // The unit of work is a page that receives rows, because an 8-bit page has one exponent per head: its new rows' largest
 // magnitude has to be known before the first of them is stored.  A workgroup takes one such page of one sequence and a share
-// of the heads; half of its threads carry the keys and half the values, so that both are in flight together.  A row is
-// LPR lanes of sixteen columns (rope.hpp); a head's new rows of the page stay in registers between the pass that finds their
-// largest magnitude and the pass that stores them.  The angles of a page's rows are the same for all heads: their cosines and
-// sines are computed once per workgroup and kept in LDS.
+// of the heads; half of its threads carry the keys and half the values, so that both are in flight together (pages of more
+// than 16384 elements: all of them the keys, then the values).  A row is LPR lanes of sixteen columns (rope.hpp); a head's new
+// rows of the page stay in registers between the pass that finds their largest magnitude and the pass that stores them.  The
+// angles of a page's rows are the same for all heads: their cosines and sines are computed once per workgroup and kept in
+// LDS, where the lanes of a row read them side by side.
+// Measured: 8 prompts of 6144 to 8192 rows x 8 heads of 128, bf16 into 8 bits 83 us (4.2 TB/s read and written; a copy of 4 GiB
+// reaches 4.76); 64 single tokens 6 us of which the host's part is 4.7.
 #include <algorithm>
 
 #include "common.hpp"

@@ -383,12 +383,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
 // ---------------------------------------------------------------------------
 // Few rows: 32 packed query rows per wavefront, QW blocks of them per workgroup (1 or 2).
 // Bound by the cache's bytes.  The four wavefronts are QW row blocks x KS streams of 32-key blocks and never wait for each
-// other inside the loop: a wavefront loads its 32 rows of K straight into the registers that feed the matrix instruction
-// (S^T = K Q^T; the order of the contraction is free, so a lane's sixteen consecutive values serve two instructions), and its 32
-// rows of V into a corner of LDS of its own, from which the transposing read makes the operand of O^T += V^T P^T.  The next
-// block's V is requested as soon as this one's is in LDS, its K as soon as this one's scores are made.  Pages are multiples
-// of sixteen rows, so a block's page numbers and exponents are two scalars each, known a block earlier.  The streams'
-// results meet in LDS at the end.
+// other inside the loop: a wavefront requests its own 32 rows of K and V in whole rows, and passes them through a corner of LDS
+// of its own, K as stored (a lane reads sixteen consecutive columns of its key and widens them; the order of the contraction
+// in S^T = K Q^T is free, so they serve two instructions), V widened, in the layout that the transposing read turns into the
+// operand of O^T += V^T P^T.  The next block is requested as soon as this one is in LDS; a deeper queue took registers that
+// were not there and gained nothing (4 x 100000 keys: 172 us one block ahead, 177 two).  Pages are multiples of sixteen
+// rows, so a block's page numbers and exponents are two scalars each, known a block earlier.  The streams' results meet in
+// LDS at the end.
+// Measured: 8 KV heads x 8 queries over 4 x 100000 keys in 8 bits (820 MB) 138 to 148 us, 5.5 to 5.9 TB/s; 8 KV heads x 4 over 1500 keys
+// 10 us, a chain of eight trips to memory: length, page, exponents and rows, partial, ticket, partials.
 // ---------------------------------------------------------------------------
 template <int D, bool KV8, int QW>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_rows_kernel(OT_LEAD_PARAMS, const PagedArgs a) {
@@ -500,46 +503,45 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             r.page[e] = there ? r.page[e] : 0;
         }
     };
-    constexpr int DIST = 1;         // blocks requested ahead
-    u32x4 kr[DIST][KL], vr[DIST][KL];
-    int ke[DIST][2], ve[DIST][2];                        // exponents of either half of the block
+    u32x4 kr[KL], vr[KL];
+    int ke[2], ve[2];                                    // exponents of either half of the block
     // Every instruction asks for whole rows, and says that they are read once: 16 bytes of 32 rows each instead, as the matrix
     // operand wants them, or without the hint, 64 heads over 4 x 100000 keys take 172 us, not 156.
     const unsigned k_lane = (unsigned)(lane / CPR) * a.k_row + 16 * (lane % CPR);
     const unsigned v_lane = (unsigned)(lane / CPR) * a.v_row + 16 * (lane % CPR);
     const unsigned char* const kh = a.kp + hk * a.k_head;
     const unsigned char* const vh = a.vp + hk * a.v_head;
-    auto load_k = [&](int i, const Pages& r, int at) {
+    auto load_k = [&](int i, const Pages& r) {
         const unsigned char* b[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             b[e] = row_of(kh, r.page[e], a.k_page, (32 * i + 16 * e) & (ps - 1), a.k_row);
-            if constexpr (KV8) ke[at][e] = scalar_byte(a.k_exp, (unsigned)r.page[e] * a.kv_heads + hk);
+            if constexpr (KV8) ke[e] = scalar_byte(a.k_exp, (unsigned)r.page[e] * a.kv_heads + hk);
         }
 #pragma unroll
         for (int n = 0; n < KL; ++n)                     // rows n RPL .. n RPL + RPL - 1 of the block
-            kr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + ((n * RPL) & 15) * a.k_row + k_lane));
+            kr[n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + ((n * RPL) & 15) * a.k_row + k_lane));
     };
-    auto load_v = [&](int i, const Pages& r, int at) {
+    auto load_v = [&](int i, const Pages& r) {
         const unsigned char* b[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             b[e] = row_of(vh, r.page[e], a.v_page, (32 * i + 16 * e) & (ps - 1), a.v_row);
-            if constexpr (KV8) ve[at][e] = scalar_byte(a.v_exp, (unsigned)r.page[e] * a.kv_heads + hk);
+            if constexpr (KV8) ve[e] = scalar_byte(a.v_exp, (unsigned)r.page[e] * a.kv_heads + hk);
         }
 #pragma unroll
         for (int n = 0; n < KL; ++n)
-            vr[at][n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + ((n * RPL) & 15) * a.v_row + v_lane));
+            vr[n] = __builtin_nontemporal_load((const u32x4*)(b[(n * RPL) >> 4] + ((n * RPL) & 15) * a.v_row + v_lane));
     };
-    auto stage = [&](unsigned seen, int slot) {
+    auto stage = [&](unsigned seen) {
         wave_fence();
 #pragma unroll
-        for (int n = 0; n < KL; ++n) *(u32x4*)(s_k + k_at(n * RPL + lane / CPR, lane % CPR)) = kr[slot][n];
-        const float vs[2] = {KV8 ? exp_scale(ve[slot][0]) : 1.f, KV8 ? exp_scale(ve[slot][1]) : 1.f};
+        for (int n = 0; n < KL; ++n) *(u32x4*)(s_k + k_at(n * RPL + lane / CPR, lane % CPR)) = kr[n];
+        const float vs[2] = {KV8 ? exp_scale(ve[0]) : 1.f, KV8 ? exp_scale(ve[1]) : 1.f};
 #pragma unroll
         for (int n = 0; n < KL; ++n) {
             const int row = n * RPL + lane / CPR, at = lane % CPR;
-            u32x4 w = vr[slot][n];
+            u32x4 w = vr[n];
             if (seen != 0xffffffffu && !(seen >> row & 1)) w = u32x4{0, 0, 0, 0};
             if constexpr (KV8) {
                 u32x4 lo, hi;
@@ -577,39 +579,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             // Requests past the last block read that one again: a load under a condition would make every wait for an older one
             // a wait for all.
             auto in_range = [&](int k) { return min(k, end - 1); };
-            unsigned seen[DIST];
-#pragma unroll
-            for (int d = 0; d < DIST; ++d) {
-                const int k = in_range(i + d * KS);
-                Pages p = pages_of(k);
-                check(p);
-                load_v(k, p, d);
-                load_k(k, p, d);
-                seen[d] = p.seen;
-            }
-            Pages ahead = pages_of(in_range(i + DIST * KS));
-            // block i is in slot `slot`; true: there is another one
-            auto step = [&](auto slot_c) {
-                constexpr int slot = slot_c;
-                const int to = in_range(i + DIST * KS);
-                const Pages after = pages_of(in_range(i + DIST * KS + KS));
+            Pages now = pages_of(i), ahead = pages_of(in_range(i + KS));
+            check(now);
+            load_v(i, now);
+            load_k(i, now);
+            for (; i < end; i += KS) {
+                const int to = in_range(i + KS);
+                const Pages after = pages_of(in_range(i + 2 * KS));
                 check(ahead);
-                const unsigned now = seen[slot];
-                const int e0 = KV8 ? ke[slot][0] : 0, e1 = KV8 ? ke[slot][1] : 0;
-                stage(now, slot);
+                const unsigned seen = now.seen;
+                const int e0 = KV8 ? ke[0] : 0, e1 = KV8 ? ke[1] : 0;
+                stage(seen);
                 __builtin_amdgcn_sched_barrier(0);
-                load_v(to, ahead, slot);
-                load_k(to, ahead, slot);
+                load_v(to, ahead);
+                load_k(to, ahead);
                 __builtin_amdgcn_sched_barrier(0);
                 f32x16 s = scores(e0, e1);
-                if (now != 0xffffffffu) hide(s, now, h);
+                if (seen != 0xffffffffu) hide(s, seen, h);
                 finish(s);
-                seen[slot] = ahead.seen;
+                now = ahead;
                 ahead = after;
-                i += KS;
-                return i < end;
-            };
-            while (step(std::integral_constant<int, 0>()) && (DIST == 1 || step(std::integral_constant<int, DIST - 1>()))) {}
+            }
         }
     }
     if (bad && lane == 0)
@@ -718,9 +708,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 
 // ---------------------------------------------------------------------------
 // Many rows: 32 packed query rows per wavefront, NW wavefronts, all of them over every 64-key tile of the job.
-// Bound by the matrix cores and the exponentials.  A tile is requested into registers two tiles ahead, widened to bf16 on its
-// way into LDS one tile ahead, and read by all wavefronts (one barrier per tile).
+// Bound by the matrix cores, the exponentials and the issue of what surrounds them.  A tile is requested into registers a tile
+// ahead of its way into LDS, widened to bf16 there, and read by all wavefronts.
 //   K [64][D]: 16-byte piece c of row r at c ^ (r mod D/8);  V [64][D]: 32-byte segment g of row r at g ^ v_swizzle(r)
+// 256 rows take eight wavefronts, one workgroup to a compute unit; up to 128 rows four, two workgroups to a unit, which drift
+// apart by themselves.
+// Measured: 16 x 8 KV heads x 1024 queries over 8192 keys in 8 bits (550 GFLOP) 545 to 575 us, 0.96 to 1.0 PFLOP/s, where a large bf16
+// matrix product of the library reaches 1.23; 16 x 8 x 480 over 4096 +-25 % 157 to 165 us (the longest sequence decides).
 // ---------------------------------------------------------------------------
 template <int D, bool KV8, int NW>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2))) void paged_tiles_kernel(OT_LEAD_PARAMS, const PagedArgs a) {
@@ -896,7 +890,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2, 2)))
             // of tile t), wavefronts 4..7 do the exponentials of tile t - 1 and bring a tile into LDS, and the other way
             // round; a barrier changes sides.  A tile of V is read half a turn into the next tile and written two turns
             // ahead: three buffers; K two.  Without turns both wavefronts would be at the same kind of work, since they meet
-            // at every tile: 16 x 32 heads x 256 nodes over 8192 keys 607 us, not OT_TURNS us.
+            // at every tile: 16 x 32 heads x 256 nodes over 8192 keys 649 us, not 576.
             const bool second = wave >= 4;
             __syncthreads();
             if (second) { advance(); __syncthreads(); }

@@ -6,6 +6,8 @@
 // its heads): the angles of a token are the same for all of its heads, so their cosines and sines are computed once, a
 // thread each, and kept in LDS.  A row is eight lanes (head_dim 64: four) of sixteen columns, so its norm is three
 // (two) exchanges inside a row of sixteen lanes and both partners of a pair are in one lane (rope.hpp).
+// Measured: 15009 tokens x 40 heads of 128 in fp32 (615 MB) 130 us, 4.7 TB/s, the rate of a plain copy; 960 tokens x 72 heads in bf16
+// (35 MB) 9.4 us; one token x 40 heads 2.8 us on the card, 5.7 a call.
 #include <algorithm>
 
 #include "common.hpp"
@@ -133,6 +135,7 @@ int ot_qk_norm_rope(const ot_qk_params* p, const void* Q, const void* K, const v
     a.shift = p->shift; a.eps = p->eps;
     for (int i = 0; i < 3; ++i) { a.qs[i] = p->q_strides[i]; a.ks[i] = p->k_strides[i]; a.qos[i] = p->qo_strides[i]; a.kos[i] = p->ko_strides[i]; }
     const int rpp = kThreads * 16 / p->head_dim;
+    // two passes of rows per workgroup (four: 149 us, not 130, at 15009 tokens x 40 heads in fp32)
     a.tokens = std::min(kMaxTokens, std::max(1, 2 * rpp / a.heads));
     a.share = a.heads;
     if ((a.all_tokens + a.tokens - 1) / a.tokens < 512) {      // few tokens: a token each, heads over several workgroups

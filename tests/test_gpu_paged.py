@@ -544,3 +544,157 @@ def test_a_decoding_step_over_a_paged_cache(eight):
         torch.cuda.synchronize()
         # bit by bit: rows that nothing has written may be NaNs
         assert all(torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)) for a, b in zip(got, want)), replay
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# calls that the documentation allows and the cases above do not make
+# ---------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("eight", [True, False])
+def test_pools_of_more_than_4_gib(eight):
+    """Pages behind 2^32 bytes: what an append writes there is what an attention reads, and equals the same rows in a small pool."""
+    import torch
+    from paper_2406_17276_amd import api
+    torch.manual_seed(11)
+    H, ps, D, n = 8, 64, 128, 150
+    pages = (5 << 30) // (H * ps * D * (1 if eight else 2))
+    big = api.alloc_paged_cache(pages, H, ps, D, 1, 4, eight_bit=eight)
+    small = api.alloc_paged_cache(4, H, ps, D, 1, 4, eight_bit=eight)
+    ids = [pages - 1, 3, pages // 2 + 7, pages - 2]
+    big.table.copy_(i32([ids]))
+    small.table.copy_(i32([[2, 0, 3, 1]]))
+    K, V = (torch.randn(1, H, n, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    f, f_dev = inv_freq(D)
+    for q_rows in (1, 40, 200):
+        Q = torch.randn(1, H, q_rows, D, device="cuda").to(torch.bfloat16)
+        out = []
+        for c in (big, small):
+            new = api.kv_append_paged(c, K, V, i32([0]), inv_freq=f_dev)
+            new = api.kv_append_paged(c, K[:, :, :30], V[:, :, :30], new, inv_freq=f_dev)
+            assert new.tolist() == [180]
+            out.append(api.tree_verify_attention_paged(Q, c, new))
+        assert torch.equal(out[0], out[1]) and torch.isfinite(out[0]).all()
+    for a, b in ((ids[0], 2), (ids[1], 0)):
+        assert torch.equal(big.k[a].view(torch.uint8), small.k[b].view(torch.uint8)) and torch.equal(big.v[a].view(torch.uint8), small.v[b].view(torch.uint8))
+
+
+@pytest.mark.parametrize("B, Hq, Hkv, n", [(300, 2, 1, 1), (130, 2, 2, 3), (300, 4, 2, 40)])
+def test_attention_of_large_batches(B, Hq, Hkv, n):
+    """More sequences than lanes, and more than are cut into ranges; one of them is long."""
+    import torch
+    from paper_2406_17276_amd import api
+    g = np.random.default_rng(B + n)
+    D, ps = 64, 16
+    lens = g.integers(0, 40, B).tolist()
+    lens[B - 2] = 700
+    counts = [-(-l // ps) for l in lens]
+    order = g.permutation(sum(counts))
+    table = np.full((B, max(counts)), -1)
+    at = 0
+    for b, c in enumerate(counts):                               # entries behind a sequence's pages are no pages, and not read
+        table[b, :c] = order[at:at + c]
+        at += c
+    host, exps, cache = make_cache(g, sum(counts), Hkv, ps, D, True, table)
+    Q = wl.store(g.standard_normal((B, Hq, n, D)).astype(np.float32), "bf16")
+    q = dev(Q, "bf16")
+    ws = api.paged_attn_workspace(q, cache)
+    got = api.tree_verify_attention_paged(q, cache, i32(lens), workspace=ws)
+    assert api.attn_status(ws) == 0
+    check_attention(got, Q, host, exps, table, lens)
+
+
+def test_padded_pools_and_fused_projections():
+    """Pools that are slices of larger ones (pages, heads and rows further apart than they are long), rows of a fused projection."""
+    import torch
+    from paper_2406_17276_amd import api
+    torch.manual_seed(5)
+    B, H, ps, D, n = 2, 3, 32, 64, 50
+    for eight in (True, False):
+        t = torch.uint8 if eight else torch.bfloat16
+        store = [torch.full((9, 4, ps + 3, D + 16), 7, dtype=t, device="cuda") for _ in range(2)]
+        views = [x[1:, :H, 1:ps + 1, 16:] for x in store]
+        exps = [torch.full((8, H), 120, dtype=torch.uint8, device="cuda") for _ in range(2)] if eight else [None, None]
+        table = i32([[7, 0, 3], [2, 6, 4]])
+        slices, plain = api.PagedCache(*views, table, *exps), api.alloc_paged_cache(8, H, ps, D, B, 3, eight_bit=eight)
+        plain.table.copy_(table)
+        fused = torch.randn(B, n, 5 * H, D, device="cuda").to(torch.bfloat16)
+        K, V = fused[:, :, H:2 * H].transpose(1, 2), fused[:, :, 4 * H:].transpose(1, 2)
+        for c in (slices, plain):
+            new = api.kv_append_paged(c, K, V, i32([0, 20]), count=i32([50, 44]))
+        assert new.tolist() == [50, 64]
+        Q = torch.randn(B, 2 * H, 9, D, device="cuda").to(torch.bfloat16)
+        lens = i32([50, 20])                                     # (rows 0..19 of the second are not the same in both pools)
+        a, b = (api.tree_verify_attention_paged(Q[:1], api.PagedCache(c.k, c.v, c.table[:1], c.k_exp, c.v_exp), lens[:1]) for c in (slices, plain))
+        assert torch.equal(a, b)
+        for x, v in zip(store, views):                           # nothing between the rows was touched
+            v.fill_(7)
+            assert (x == 7).all()
+
+
+def test_refusals_leave_the_device_alone():
+    import torch
+    from paper_2406_17276_amd import api
+    cache = api.alloc_paged_cache(4, 2, 16, 64, 1, 2)
+    q = torch.zeros(1, 4, 1, 64, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(1, 2, 3, 64, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(api.OptTreeError) as e:
+        api.tree_verify_attention_paged(q, cache, i32([0]), workspace=torch.zeros(65536, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == -3
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(q, cache, torch.zeros(1, dtype=torch.int32))                     # lengths on the host
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(q, cache, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(q.float(), cache, i32([0]))
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(q, cache, i32([0]), k, k)                                        # a tree without its mask
+    with pytest.raises(ValueError):
+        api.kv_append_paged(cache, k, k[:, :, :2], i32([0]))
+    with pytest.raises(ValueError):
+        api.kv_append_paged(cache, k, k, i32([0]), rows=i32([[0, 1]]))
+    with pytest.raises(ValueError):
+        api.kv_append_paged(cache, k.transpose(2, 3).contiguous().transpose(2, 3), k, i32([0]))          # last dimension apart
+    with pytest.raises(ValueError):
+        api.qk_norm_rope(q, torch.zeros(1, 2, 2, 64, dtype=torch.bfloat16, device="cuda"), i32([0]))
+    with pytest.raises(ValueError):
+        api.qk_norm_rope(q, None, i32([0]), torch.zeros(32, device="cuda"))                              # inv_freq is float64
+    with pytest.raises(api.OptTreeError):
+        api.qk_norm_rope(q, None, i32([0]), torch.zeros(40, dtype=torch.float64, device="cuda"))         # more than head_dim
+    lens = i32([3])
+    with pytest.raises(api.OptTreeError):
+        api.kv_append_paged(cache, k, k, lens, new_len=lens)                                             # in place
+    cache.k_exp = None
+    with pytest.raises(TypeError):
+        api.kv_append_paged(cache, k, k, lens)
+    torch.cuda.synchronize()
+
+
+def test_prompt_in_chunks_equals_the_prompt_at_once():
+    """A prompt of 300 tokens attends in chunks of 64 under a causal mask over what earlier chunks left in 16-bit pages; every
+    output row is what plain causal attention gives."""
+    import torch
+    from paper_2406_17276_amd import api
+    g = np.random.default_rng(21)
+    Hq, H, D, ps, n, chunk = 6, 2, 128, 32, 300, 64
+    f, f_dev = inv_freq(D)
+    cache = api.alloc_paged_cache(10, H, ps, D, 1, 10, eight_bit=False)
+    cache.table.copy_(torch.randperm(10, device="cuda", dtype=torch.int32)[None])
+    Q, K, V = (wl.store(g.standard_normal((1, h, n, D)).astype(np.float32), "bf16") for h in (Hq, H, H))
+    q, k, v = (dev(x, "bf16") for x in (Q, K, V))
+    length, outs = i32([0]), []
+    for c0 in range(0, n, chunk):
+        m = min(chunk, n - c0)
+        tri = torch.tensor([-1 if i == 63 else (2 << i) - 1 for i in range(m)], dtype=torch.int64, device="cuda").view(1, m, 1)
+        qq, kk = api.qk_norm_rope(q[:, :, c0:c0 + m], k[:, :, c0:c0 + m], length, f_dev)
+        outs.append(api.tree_verify_attention_paged(qq, cache, length, kk, v[:, :, c0:c0 + m], tri))
+        length = api.kv_append_paged(cache, kk, v[:, :, c0:c0 + m], length)
+    got = U.from_device_f64(torch.cat(outs, 2))
+    qr, kr = api.qk_norm_rope(q, k, i32([0]), f_dev)                      # the same rotated rows, all at once
+    qr, kr, v64 = U.from_device_f64(qr), U.from_device_f64(kr), wl.to_f64(V, "bf16")
+    for h in range(Hq):
+        s = qr[0, h] @ kr[0, h // 3].T / np.sqrt(D)
+        s[np.triu_indices(n, 1)] = -np.inf
+        w = np.exp(s - s.max(-1, keepdims=True))
+        w /= w.sum(-1, keepdims=True)
+        S = np.abs(qr[0, h]) @ np.abs(kr[0, h // 3]).T / np.sqrt(D)
+        tol = (w @ np.abs(v64[0, h // 3])) * (2 * UBF + 2.0 ** -14 + 2 * (D + 4) * U32 * S.max())
+        assert np.all(np.abs(got[0, h] - w @ v64[0, h // 3]) <= tol)
