@@ -48,13 +48,13 @@ constexpr float kSlack = 8.f;
 // wavefront start (kernel-argument preload).
 struct Lead {
     const int32_t *prefix_len, *table;
-    int batch, units, max_pages, ps_log2, tiles_tree;
+    int batch, kv_heads, row_blocks, max_pages, ps_log2, tiles_tree;
     int target;                  // jobs aimed at; 0: every sequence in one piece
     float apart;                 // what another range costs, in tiles
 };
-#define OT_LEAD_PARAMS const int32_t *l_prefix_len, const int32_t *l_table, const int l_batch, const int l_units, const int l_max_pages, \
-                       const int l_ps_log2, const int l_tiles_tree, const int l_target, const float l_apart
-#define OT_LEAD Lead{l_prefix_len, l_table, l_batch, l_units, l_max_pages, l_ps_log2, l_tiles_tree, l_target, l_apart}
+#define OT_LEAD_PARAMS const int32_t *l_prefix_len, const int32_t *l_table, const int l_batch, const int l_kv_heads, const int l_row_blocks, \
+                       const int l_max_pages, const int l_ps_log2, const int l_tiles_tree, const int l_target, const float l_apart
+#define OT_LEAD Lead{l_prefix_len, l_table, l_batch, l_kv_heads, l_row_blocks, l_max_pages, l_ps_log2, l_tiles_tree, l_target, l_apart}
 
 struct PagedArgs {
     const void *Q, *Kt, *Vt;
@@ -111,22 +111,24 @@ struct Job {
 // fewest with which all jobs together are no more than `target`, and at least sqrt(T apart), T the tiles of the longest
 // sequence: S ranges take T / S tiles and S joins of `apart` tiles each, which is least there.  Each sequence takes
 // ceil(tiles / share) ranges of equal length.  Lane j holds sequences j, j + 64, ...
+// Workgroups go to XCD wg % 8 in order; the row blocks of a KV head and range, which read the same rows, take consecutive
+// places on one XCD, whose L2 they share (16 x 8 KV heads x 4 row blocks over 8192 keys: 535 us, not 545).
 __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int wg) {
     const int lane = threadIdx.x & 63, cap = a.max_pages << a.ps_log2;
+    const int units = a.kv_heads * a.row_blocks, place = wg >> 3, group = place / a.row_blocks;
+    const int pair = group * 8 + (wg & 7), u = pair / a.kv_heads;        // KV head of u: a sequence, or a (sequence, range)
     Job j;
     j.none = false;
+    j.unit = (pair - u * a.kv_heads) * a.row_blocks + place - group * a.row_blocks;
     int raw;
     if (!a.target) {
-        j.b = wg / a.units;
-        j.unit = wg - j.b * a.units;
+        j.b = u;
         j.splits = 1; j.split = 0; j.slot = 0;
         if (j.b >= a.batch) { j.none = true; return j; }
         raw = a.prefix_len[j.b];
     } else {
         constexpr int NL = kSplitBatch / 64;
         const int target = a.target;
-        const int u = wg / a.units;                      // which (sequence, range)
-        j.unit = wg - u * a.units;
         int len[NL], T[NL], S[NL], most = 0;
         float total = 0.f;
 #pragma unroll
@@ -141,7 +143,7 @@ __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int w
                 total += (float)wave_sum_i(T[i]);
                 most = max(most, wave_max_i(T[i]));
             }
-        int share = max(1, min(most, (int)ceilf(fmaxf(total * (float)a.units / (float)target, sqrtf((float)most * a.apart)))));
+        int share = max(1, min(most, (int)ceilf(fmaxf(total * (float)units / (float)target, sqrtf((float)most * a.apart)))));
         int jobs;
         while (true) {
             jobs = 0;
@@ -151,7 +153,7 @@ __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int w
                     S[i] = lane + 64 * i < a.batch ? max(1, (int)((unsigned)(T[i] + share - 1) / (unsigned)share)) : 0;
                     jobs += wave_sum_i(S[i]);
                 }
-            if (jobs <= target / a.units || share >= most) break;
+            if (jobs <= target / units || share >= most) break;
             share += max(1, share >> 4);
         }
         if (u >= jobs) { j.none = true; return j; }
@@ -171,7 +173,7 @@ __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int w
                 }
                 before = rl(end, 63);
             }
-        j.slot = wg - j.split * a.units;                 // of the unit's first range
+        j.slot = (u - j.split) * units + j.unit;         // of the unit's first range
     }
     raw = uniform(raw);
     j.len = min(max(raw, 0), cap);
@@ -713,7 +715,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //   K [64][D]: 16-byte piece c of row r at c ^ (r mod D/8);  V [64][D]: 32-byte segment g of row r at g ^ v_swizzle(r)
 // 256 rows take eight wavefronts, one workgroup to a compute unit; up to 128 rows four, two workgroups to a unit, which drift
 // apart by themselves.
-// Measured: 16 x 8 KV heads x 1024 queries over 8192 keys in 8 bits (550 GFLOP) 545 to 575 us, 0.96 to 1.0 PFLOP/s, where a large bf16
+// Measured: 16 x 8 KV heads x 1024 queries over 8192 keys in 8 bits (550 GFLOP) 535 to 575 us, 0.96 to 1.03 PFLOP/s, where a large bf16
 // matrix product of the library reaches 1.23; 16 x 8 x 480 over 4096 +-25 % 157 to 165 us (the longest sequence decides).
 // ---------------------------------------------------------------------------
 template <int D, bool KV8, int NW>
@@ -1016,13 +1018,15 @@ PagedPlan plan_paged(const ot_paged_attn_params& p, const ot_paged_cache& c) {
     const long long all = (long long)p.batch * pl.units;
     const int resident = pl.rows <= 128 ? 512 : 256;           // workgroups that the card holds
     pl.target = p.batch <= kSplitBatch && all < resident ? resident : 0;
-    pl.grid = pl.target ? pl.target : (int)all;
+    // workgroups: whole rounds of eight XCDs (find_job); jobs, and partials, are `target` at most
+    const long long pairs = pl.target ? pl.target / pl.row_blocks : (long long)p.batch * c.kv_heads;
+    pl.grid = (int)((pairs + 7) / 8 * 8 * pl.row_blocks);
     pl.late = pl.target && pl.slot_rows > kTicketRows;
     // A range more costs a partial written and read by every unit, at 4 TB/s, or a trip to memory for a chunk of sixteen; a
     // tile of 64 keys takes (us, head_dim 128) 0.7 for up to 64 rows, 1.2 for 128, 2.2 for 256.
     const float tile = (pl.rows <= 64 ? 0.7f : pl.rows == 128 ? 1.2f : 2.2f) * (float)c.head_dim / 128.f;
     pl.apart = (pl.late ? (float)all * (float)pl.slot_rows * (float)c.head_dim * 8.f / 4e6f + 0.02f : 0.13f) / tile;
-    const size_t jobs = pl.target ? (size_t)pl.grid : 0;
+    const size_t jobs = (size_t)pl.target;
     pl.part_bytes = jobs * pl.slot_rows * c.head_dim * 4;
     pl.ml_bytes = jobs * pl.slot_rows * 8;
     pl.bytes = OT_PAGED_SYNC_BYTES + pl.part_bytes + pl.ml_bytes + (pl.late ? (size_t)all * sizeof(int2) : 0);
@@ -1046,7 +1050,7 @@ int validate_paged(const ot_paged_attn_params* p, const ot_paged_cache* c, bool 
 
 template <int D, bool KV8>
 int launch_paged(const Lead& l, const PagedArgs& a, const PagedPlan& pl, hipStream_t s) {
-#define OT_LEAD_ARGS l.prefix_len, l.table, l.batch, l.units, l.max_pages, l.ps_log2, l.tiles_tree, l.target, l.apart
+#define OT_LEAD_ARGS l.prefix_len, l.table, l.batch, l.kv_heads, l.row_blocks, l.max_pages, l.ps_log2, l.tiles_tree, l.target, l.apart
     constexpr size_t tile = (size_t)kTile * D * 2;
     if (pl.rows == 32) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 1>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
     else if (pl.rows == 64) hipLaunchKernelGGL((paged_rows_kernel<D, KV8, 2>), dim3(pl.grid), dim3(256), 0, s, OT_LEAD_ARGS, a);
@@ -1060,7 +1064,7 @@ int launch_paged(const Lead& l, const PagedArgs& a, const PagedPlan& pl, hipStre
 #undef OT_LEAD_ARGS
     OT_HIP_CHECK(hipGetLastError());
     if (!pl.late) return OT_OK;
-    hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)((pl.slot_rows + 1024 / D - 1) / (1024 / D)), (unsigned)(l.batch * l.units)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)((pl.slot_rows + 1024 / D - 1) / (1024 / D)), (unsigned)(l.batch * pl.units)), dim3(256), 0, s, a);
     OT_HIP_CHECK(hipGetLastError());
     return OT_OK;
 }
@@ -1106,7 +1110,7 @@ int ot_tree_verify_attention_paged(const ot_paged_attn_params* p, const ot_paged
     a.tree_keys = p->tree_keys; a.W = OT_MASK_WORDS(p->tree_keys);
     a.row_blocks = pl.row_blocks; a.units = pl.units;
     a.num_pages = cache->num_pages; a.block_rows = pl.rows; a.slot_rows = pl.slot_rows;
-    const Lead lead{prefix_len, cache->page_table, p->batch, pl.units, cache->max_pages, log2_of(cache->page_size),
+    const Lead lead{prefix_len, cache->page_table, p->batch, cache->kv_heads, pl.row_blocks, cache->max_pages, log2_of(cache->page_size),
                     (p->tree_keys + kTile - 1) / kTile, pl.target, pl.apart};
     a.scale_log2 = (p->softmax_scale != 0.f ? p->softmax_scale : 1.0f / sqrtf((float)cache->head_dim)) * kLog2e;
     for (int i = 0; i < 3; ++i) {
