@@ -10,6 +10,8 @@ the HIP package.
                      Algorithm 1 with a fixed number of drafting steps)
   tree_attention.py  tree-masked attention used by the verification forward
                      (Sec. 3, Algorithm 2: the mask that goes with the tree)
+  paged.py           norms and rotation of heads, append to and attention over a
+                     paged cache
 
 Parity pins (tests/test_oracle_*.py, marker "not gpu"):
   row statistics      -> scipy.special.logsumexp, closed form for constant rows,
