@@ -478,8 +478,9 @@ def paged_params(Q, cache: PagedCache, K_tree=None, V_tree=None, softmax_scale: 
     """The C structs of an attention call (size queries, measurement, callers of the C ABI)."""
     st = lambda t: (C.c_int64 * 3)(*(t.stride()[:3] if t is not None else (0, 0, 0)))
     V_tree = K_tree if V_tree is None else V_tree
-    p = PagedAttnParams(Q.shape[0], Q.shape[1], Q.shape[2], 0 if K_tree is None else K_tree.shape[2], float(softmax_scale), st(Q),
-                        st(K_tree), st(V_tree), st(Q))
+    B, Hq, n, D = Q.shape
+    p = PagedAttnParams(B, Hq, n, 0 if K_tree is None else K_tree.shape[2], float(softmax_scale), st(Q),
+                        st(K_tree), st(V_tree), (C.c_int64 * 3)(Hq * n * D, n * D, D))                      # O in one piece
     ptr = lambda t: None if t is None else t.data_ptr()
     import torch
     P, H, ps, D = cache.k.shape

@@ -28,6 +28,10 @@ inline int sequences_per_launch(int batch, long long threads_per_sequence) {
     const long long most = 0xffffffffLL / threads_per_sequence, launches = (batch + most - 1) / most;
     return (int)((batch + launches - 1) / launches);
 }
+// Does a tensor of these sizes and strides hold the same row twice (broadcast)?  Right for what is read, a race where it is written.
+inline bool repeats(const int64_t* strides, int64_t n0, int64_t n1, int64_t n2) {
+    return (strides[0] == 0 && n0 > 1) || (strides[1] == 0 && n1 > 1) || (strides[2] == 0 && n2 > 1);
+}
 
 // Frontier sizes F_0 = 1, F_{t+1} = min(n, k F_t) and their prefix sums
 // (Algorithm 1: each drafting step keeps at most n candidates).

@@ -698,3 +698,30 @@ def test_prompt_in_chunks_equals_the_prompt_at_once():
         S = np.abs(qr[0, h]) @ np.abs(kr[0, h // 3]).T / np.sqrt(D)
         tol = (w @ np.abs(v64[0, h // 3])) * (2 * UBF + 2.0 ** -14 + 2 * (D + 4) * U32 * S.max())
         assert np.all(np.abs(got[0, h] - w @ v64[0, h // 3]) <= tol)
+
+
+def test_broadcast_inputs_are_read_and_broadcast_outputs_refused():
+    import torch
+    from paper_2406_17276_amd import api
+    g = np.random.default_rng(33)
+    B, Hq, H, D, ps, n = 2, 4, 2, 64, 16, 5
+    _, f_dev = inv_freq(D)
+    new = lambda *s: dev(wl.store(g.standard_normal(s).astype(np.float32), "bf16"), "bf16")
+    q, k, v, page = new(1, Hq, n, D).expand(B, -1, -1, -1), new(B, 1, n, D).expand(-1, H, -1, -1), new(B, H, 1, D).expand(-1, -1, n, -1), new(6, 1, ps, D)
+    first, lens = i32([30, 7]), i32([30, 16])
+    for a, b in zip(api.qk_norm_rope(q, k, first, f_dev), api.qk_norm_rope(q.contiguous(), k.contiguous(), first, f_dev)):
+        assert torch.equal(a, b)
+    table = i32([[4, 1, 3], [0, 5, 2]])
+    one = api.PagedCache(page.expand(-1, H, -1, -1), page.expand(-1, H, -1, -1), table)          # the heads share their keys
+    many = api.PagedCache(one.k.contiguous(), one.v.contiguous(), table)
+    mask = torch.full((B, n, 1), 31, dtype=torch.int64, device="cuda")
+    want = api.tree_verify_attention_paged(q.contiguous(), many, lens, k.contiguous(), v.contiguous(), mask)
+    assert torch.equal(api.tree_verify_attention_paged(q, one, lens, k, v, mask), want)
+    with pytest.raises(api.OptTreeError):
+        api.kv_append_paged(one, k, v, lens)
+    with pytest.raises(api.OptTreeError):
+        api.qk_norm_rope(q, None, first, f_dev, q_out=q)
+    other = api.PagedCache(many.k.clone(), many.v.clone(), table)
+    assert torch.equal(api.kv_append_paged(many, k, v, lens, inv_freq=f_dev), i32([35, 21]))
+    api.kv_append_paged(other, k.contiguous(), v.contiguous(), lens, inv_freq=f_dev)
+    assert torch.equal(many.k, other.k) and torch.equal(many.v, other.v)

@@ -106,6 +106,21 @@ def test_norm_rope_refuses(bad, status):
     assert api.lib().ot_qk_norm_rope(C.byref(_qk(**bad)), *([F] * 9), None) == status
 
 
+@pytest.mark.parametrize("stride", [(0, 192, 64), (768, 0, 64), (768, 192, 0)])
+def test_broadcast_rows_are_not_written(stride):
+    """Two rows of an output at one address would be a race; on an axis of one row a stride says nothing."""
+    L, far = api.lib(), C.c_void_p(0x900000)
+    for name in ("qo_strides", "ko_strides"):
+        assert L.ot_qk_norm_rope(C.byref(_qk(batch=2, **{name: s3(*stride)})), *([F] * 9), None) == -1, name
+    assert L.ot_tree_verify_attention_paged(C.byref(_pp(batch=2, o_strides=s3(*stride))), C.byref(_cache()), *([F] * 7), 1 << 30, None) == -1
+    assert L.ot_paged_attn_workspace_bytes(C.byref(_pp(batch=1, n=1, o_strides=s3(0, 64, 0))), C.byref(_cache())) > 0
+    for name in ("k_strides", "v_strides"):
+        for pool in ((0, 1024, 64), (2048, 0, 64)):
+            c = _cache(**{name: s3(*pool)})
+            assert L.ot_kv_append_paged(C.byref(_ap()), C.byref(c), F, F, F, F, F, F, far, None) == -1, (name, pool)
+            assert L.ot_paged_attn_workspace_bytes(C.byref(_pp()), C.byref(c)) > 0                       # is read
+
+
 def test_norm_rope_refuses_pointers():
     L, p = api.lib(), _qk()
     for i in (0, 1, 4, 5, 7, 8):                                           # Q, K, inv_freq, first, Q_out, K_out
