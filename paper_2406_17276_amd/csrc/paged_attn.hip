@@ -21,6 +21,7 @@
 namespace ot {
 namespace {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -226,6 +227,9 @@ template <int D> __device__ __forceinline__ int v_swizzle(int r) { return D == 1
 
 // NB 32-key blocks of scores (lane: query l32, keys 8 (v/4) + 4 h + v%4 of a block) become probabilities; returns them packed as the
 // B operands of the blocks' 16-key slabs, and rescales what the row has summed when the reference moves.
+// A probability is rounded to bf16, the type that the matrix cores multiply V by; the sum is taken of the rounded ones, so that the
+// weights of a row add up to one and equal values average to themselves.  Four sums side by side: two make a chain (8 x 8 KV heads of 64
+// x 200 queries over 4000 keys 43.5 us, not 42.9).
 template <int NB, int NO>
 __device__ __forceinline__ void softmax_blocks(f32x16 (&s)[NB], float c, float& ref, float& l, f32x16 (&o)[NO], u32x4 (&p)[2 * NB]) {
     // (compiler-made maxima: an assembly one would not wait for the matrix instruction that makes its operand)
@@ -242,22 +246,18 @@ __device__ __forceinline__ void softmax_blocks(f32x16 (&s)[NB], float c, float& 
             for (int v = 0; v < 16; ++v) o[d][v] *= f;
         ref = to;
     }
-    float sum[2] = {0.f, 0.f};
+    const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            s[i][v] = __builtin_amdgcn_exp2f(fmaf(s[i][v], c, -ref));
-            sum[v & 1] += s[i][v];
+        for (int v = 0; v < 16; v += 2) {
+            const bf16x2 pair = {(__bf16)__builtin_amdgcn_exp2f(fmaf(s[i][v], c, -ref)), (__bf16)__builtin_amdgcn_exp2f(fmaf(s[i][v + 1], c, -ref))};
+            sum[v >> 1 & 3] = __builtin_amdgcn_fdot2_f32_bf16(pair, ones, sum[v >> 1 & 3], false);
+            p[2 * i + (v >> 3)][v >> 1 & 3] = __builtin_bit_cast(unsigned, pair);
         }
-    l += sum[0] + sum[1];
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     asm volatile("" : "+v"(l));                          // (here, not after the next products)
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[2 * i + u][e] = pack_bf16(s[i][8 * u + 2 * e], s[i][8 * u + 2 * e + 1]);
 }
 // STEPS products whose operands come from LDS, each requested AHEAD products before it is needed and held in that order (left to
 // itself the compiler reads an operand right before its product, and every product waits for LDS).  read(i) returns the

@@ -1,0 +1,45 @@
+"""Corners of the operators around a paged cache on the GPU: what must hold exactly, or whatever lies where nobody looks."""
+import numpy as np
+import pytest
+
+import workloads as wl
+from tests import test_gpu_paged as P
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("Hq, Hkv, D, n, keys, ps, lens", [
+    (256, 256, 64, 1, 0, 16, [700, 300]), (8, 2, 64, 8, 8, 32, [400, 300]), (4, 4, 128, 40, 40, 64, [500, 129]), (6, 2, 128, 30, 30, 16, [600, 90]),
+    (128, 128, 64, 70, 70, 64, [333, 500]), (128, 128, 64, 200, 200, 64, [500, 333]), (256, 128, 128, 100, 100, 128, [300, 200])])
+def test_an_average_of_equal_rows_is_that_row(eight, Hq, Hkv, D, n, keys, ps, lens):
+    """Weights that divide by their own sum average a value to itself.  Rows of V that are all the same: products are exact in fp32, sums of N
+    positive terms and the merges are off by less than 2 N 2^-24 + 2^-14 < 2^-12 (N <= 1000), and a bf16 value stays itself under errors below
+    2^-9, so the output is V to the last bit.  (A sum of weights that are not those of the products is off by up to 2^-8.)"""
+    import torch
+    from paper_2406_17276_amd import api
+    g = np.random.default_rng(n + D)
+    B = len(lens)
+    most = max(-(-l // ps) for l in lens)
+    table = P.random_table(g, B, most, B * most)
+    host, exps, cache = P.make_cache(g, B * most, Hkv, ps, D, eight, table)
+    row = wl.store((1 + g.random(D)).astype(np.float32), "bf16")
+    row[:4] = wl.store(np.float32([1, 1.9921875, 1.0078125, 1.5]), "bf16")
+    if eight:
+        q = wl.f32_to_e4m3_bits(wl.to_f64(row, "bf16").astype(np.float32) * 64)
+        row = wl.store(wl.e4m3_bits_to_f32(q) / 64, "bf16")              # 2^(121 - 127)
+        cache.v.copy_(P.dev(np.broadcast_to(q, host[1].shape), "u8"))
+        cache.v_exp.fill_(121)
+    else:
+        cache.v.copy_(P.dev(np.broadcast_to(row, host[1].shape), "bf16"))
+    Q = P.dev(wl.store((g.standard_normal((B, Hq, n, D)) * 3).astype(np.float32), "bf16"), "bf16")
+    Kt = Vt = mask = None
+    if keys:
+        Kt = P.dev(wl.store(g.standard_normal((B, Hkv, keys, D)).astype(np.float32), "bf16"), "bf16")
+        Vt = P.dev(np.broadcast_to(row, (B, Hkv, keys, D)), "bf16")
+        mask = P.U.mask_to_device(P.tree_masks(g, B, n, keys, "tree"))
+    if eight:
+        cache.k_exp.fill_(120)                                           # keys of about 0.7: scores some 3 apart
+    got = api.tree_verify_attention_paged(Q, cache, P.i32(lens), Kt, Vt, mask)
+    want = P.dev(np.broadcast_to(row, got.shape), "bf16")
+    assert torch.equal(got, want), (int((got != want).sum()), got.numel())
