@@ -442,7 +442,7 @@ OT_API int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* c
  *   tree rows j with bit j of mask[b][i];  a query that sees nothing yields zeros.
  * Every input may be broadcast (a stride of 0), O may not (OT_ERR_INVALID_ARG) and must not overlap an input.
  * Cache rows from prefix_len[b] on and tree rows that no query of their sequence sees may hold anything, infinities and NaNs
- * included; tree rows that some query sees must be finite.  |scale * log2(e) * Q.K| stays below 2^31.
+ * included; tree rows that some query sees must be finite.  Mask bits from tree_keys on mean nothing.  |scale * log2(e) * Q.K| stays below 2^31.
  * prefix_len[b] is clamped to [0, max_pages * page_size] and rows of table entries that are no pages are left out (not seen
  * by any query); both are reported in the status word of the workspace (OT_ATTN_STATUS_PREFIX_CLAMPED,
  * OT_ATTN_STATUS_BAD_PAGE at OT_ATTN_STATUS_OFFSET; api: attn_status).

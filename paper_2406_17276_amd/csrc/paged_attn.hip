@@ -616,7 +616,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         const unsigned short* const vt = (const unsigned short*)a.Vt + (long long)j.b * a.vts[0] + (long long)hk * a.vts[1];
         for (int i = 2 * tt0 + ks; i < 2 * tt1 && 32 * i < a.tree_keys; i += KS) {
             const int last = a.tree_keys - 1;
-            const unsigned any = (unsigned)(s_union[(i >> 1) - tt0] >> (32 * (i & 1)));
+            const unsigned tail = 32 * i + 32 <= a.tree_keys ? 0xffffffffu : (1u << (a.tree_keys - 32 * i)) - 1;      // rows that exist
+            const unsigned any = (unsigned)(s_union[(i >> 1) - tt0] >> (32 * (i & 1))) & tail;
             const unsigned short* const k1 = kt + (long long)min(32 * i + l32, last) * a.kts[2] + 16 * h;
             u32x4 k[2 * NJ];
 #pragma unroll
@@ -639,7 +640,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
             for (int v = 0; v < 16; ++v) s[v] = 0.f;
 #pragma unroll
             for (int n = 0; n < 2 * NJ; ++n) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[n]), q_frag(n), s, 0, 0, 0);
-            const unsigned tail = 32 * i + 32 <= a.tree_keys ? 0xffffffffu : (1u << (a.tree_keys - 32 * i)) - 1;
             hide(s, (unsigned)(a.mask[mask_at + (i >> 1)] >> (32 * (i & 1))) & tail, h);
             finish(s);
         }

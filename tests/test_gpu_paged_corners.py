@@ -43,3 +43,27 @@ def test_an_average_of_equal_rows_is_that_row(eight, Hq, Hkv, D, n, keys, ps, le
     got = api.tree_verify_attention_paged(Q, cache, P.i32(lens), Kt, Vt, mask)
     want = P.dev(np.broadcast_to(row, got.shape), "bf16")
     assert torch.equal(got, want), (int((got != want).sum()), got.numel())
+
+
+@pytest.mark.parametrize("eight", [True, False])
+@pytest.mark.parametrize("Hq, Hkv, D, n, keys", [(2, 2, 128, 1, 37), (2, 1, 64, 20, 20), (2, 2, 128, 40, 90), (2, 1, 128, 50, 100), (2, 1, 128, 120, 120)])
+def test_mask_bits_behind_the_last_tree_row_mean_nothing(eight, Hq, Hkv, D, n, keys):
+    """Every bit of the last word from tree_keys on is set; the last tree row, which no query sees, is NaNs and infinities."""
+    import torch
+    from paper_2406_17276_amd import api
+    g = np.random.default_rng(keys)
+    table = P.random_table(g, 2, 6, 12)
+    lens = [70, 0]
+    host, exps, cache = P.make_cache(g, 12, Hkv, 16, D, eight, table)
+    Q, Kt, Vt = (wl.store(g.standard_normal((2, h, r, D)).astype(np.float32), "bf16") for h, r in ((Hq, n), (Hkv, keys), (Hkv, keys)))
+    mask = P.tree_masks(g, 2, n, keys, "random")
+    mask[:, :, -1] &= ~np.uint64(1 << (keys - 1) % 64)
+    mask[:, 0, 0] |= np.uint64(1)
+    Kt[:, :, -1] = Vt[:, :, -1] = 0
+    run = lambda k, v, m: api.tree_verify_attention_paged(P.dev(Q, "bf16"), cache, P.i32(lens), P.dev(k, "bf16"), P.dev(v, "bf16"), P.U.mask_to_device(m))
+    want = run(Kt, Vt, mask)
+    P.check_attention(want, Q, host, exps, table, lens, Kt, Vt, mask)
+    Kt[:, :, -1], Vt[:, :, -1] = 0x7fc0, 0x7f80
+    Vt[:, :, -1, ::2] = 0x7fc0
+    mask[:, :, -1] |= np.uint64(-(1 << keys % 64) & (1 << 64) - 1)
+    assert torch.equal(run(Kt, Vt, mask), want)
