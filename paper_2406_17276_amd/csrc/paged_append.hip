@@ -10,7 +10,7 @@
 // rows of the page stay in registers between the pass that finds their largest magnitude and the pass that stores them.  The
 // angles of a page's rows are the same for all heads: their cosines and sines are computed once per workgroup and kept in
 // LDS, where the lanes of a row read them side by side.
-// Measured: 8 prompts of 6144 to 8192 rows x 8 heads of 128, bf16 into 8 bits 83 us (4.2 TB/s read and written; a copy of 4 GiB
+// Measured: 8 prompts of 6144 to 8192 rows x 8 heads of 128, bf16 into 8 bits 83.7 us (4.2 TB/s read and written; a copy of 4 GiB
 // reaches 4.76); 64 single tokens 6 us of which the host's part is 4.7.
 #include <algorithm>
 
@@ -43,12 +43,19 @@ __device__ __forceinline__ int exponent_for(float top) {
 }
 __device__ __forceinline__ float power_of(int e) { return __uint_as_float((unsigned)e << 23); }   // 2^(e - 127), e in 1..254
 
-// max(a, |b|, |c|); a NaN loses
-__device__ __forceinline__ float max3_abs(float a, float b, float c) {
-    float r;
-    asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
+// Largest magnitude of values taken one by one, on their bits: as signed numbers the positive ones lie in order, as unsigned ones
+// the negative ones above all others.  (A floating-point maximum forgets what it had when it meets a signalling NaN.)
+struct Largest {
+    int pos = 0;
+    unsigned neg = 0;
+    __device__ __forceinline__ void take(float x, float y) {
+        pos = max(max(pos, __float_as_int(x)), __float_as_int(y));
+        neg = max(max(neg, __float_as_uint(x)), __float_as_uint(y));
+    }
+    __device__ __forceinline__ float magnitude() const {                 // infinity if there was one, or a NaN
+        return __uint_as_float(min(max((unsigned)pos, neg & 0x7fffffffu), 0x7f800000u));
+    }
+};
 // |x| of finite x, 0 otherwise
 __device__ __forceinline__ float finite_abs(float x) {
     const unsigned u = __float_as_uint(x) & 0x7fffffffu;
@@ -136,7 +143,7 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
     }
     for (int h = blockIdx.y * a.share; h < h1; ++h) {
         float xa[PASSES][8], xb[PASSES][8];
-        float top = 0.f;
+        Largest largest;
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
 #pragma unroll
@@ -156,12 +163,12 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
             }
             if constexpr (KV8) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = max3_abs(top, xa[p][e], xb[p][e]);
+                for (int e = 0; e < 8; ++e) largest.take(xa[p][e], xb[p][e]);
             }
         }
         unsigned char* const row_base = dst + ((long long)page * ds[0] + (long long)h * ds[1]) * ESZ;
         float f = 1.f;
-        bool infinite = false;
+        bool not_finite = false;
         if constexpr (KV8) {
             // over the wavefronts of the keys or the values, and over all
             constexpr int HW = TOGETHER ? NT / 128 : NT / 64;
@@ -176,10 +183,9 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
                 all = fmaxf(k, w);
                 return TOGETHER && val ? w : k;
             };
-            float all;
-            top = over(top, all);
-            infinite = all > 3.402823466e38f;
-            if (infinite) {                                        // the exponent is that of the finite values
+            float all, top = over(largest.magnitude(), all);
+            not_finite = all > 3.402823466e38f;
+            if (not_finite) {                                      // the exponent is that of the finite values
                 top = 0.f;
 #pragma unroll
                 for (int p = 0; p < PASSES; ++p)
@@ -208,7 +214,7 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
                 e = max(e, e_old);
             }
             f = power_of(254 - e);
-            if (infinite) {
+            if (not_finite) {
 #pragma unroll
                 for (int p = 0; p < PASSES; ++p)
 #pragma unroll

@@ -67,3 +67,41 @@ def test_mask_bits_behind_the_last_tree_row_mean_nothing(eight, Hq, Hkv, D, n, k
     Vt[:, :, -1, ::2] = 0x7fc0
     mask[:, :, -1] |= np.uint64(-(1 << keys % 64) & (1 << 64) - 1)
     assert torch.equal(run(Kt, Vt, mask), want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D, ps, rotary", [(128, 16, 0), (64, 64, 0), (128, 256, 64), (64, 16, 32)])
+def test_signalling_nans_hide_no_value(dtype, D, ps, rotary):
+    """NaNs whose quiet bit is clear reach the maxima of V, and of key columns that are not turned, as they are: behind larger values
+    of their lane, in either run of its columns, in the last place.  They are stored as NaNs and change nothing else."""
+    import torch
+    from paper_2406_17276_amd import api
+    g = np.random.default_rng(D + ps)
+    H, n = 2, 20
+    pages = -(-(n + 3) // ps)
+    table = np.arange(pages)[None]
+    host, exps, cache = P.make_cache(g, pages, H, ps, D, True, table)
+    for e in exps:
+        e[:] = 100                                                       # the older rows' exponent: well below what comes
+    cache.k_exp.fill_(100)
+    cache.v_exp.fill_(100)
+    bits = np.uint16 if dtype == "bf16" else np.uint32
+    nans = np.array([0x7f81, 0xffbf] if dtype == "bf16" else [0x7f800001, 0xffbfffff], dtype=bits)
+    stored = []
+    for turned in (rotary, 0):                                           # K, V
+        x = wl.store((g.standard_normal((1, H, n, D)) * 0.1).astype(np.float32), dtype)
+        raw = x.view(bits)
+        x64 = wl.to_f64(x, dtype)
+        for h in range(H):                                               # per head: a large value, then the NaN in its lane
+            for i, (big, at) in enumerate(((0, 3), (8, 11), (1, 15), (9, 7), (0, 8))):
+                r, c = 4 * i + h, turned + 16 * (i % ((D - turned) // 16))
+                raw[0, h, r, c + big] = wl.store(np.float32([200.0 + 10 * i + h]), dtype).view(bits)[0]
+                raw[0, h, r, c + at] = nans[i % 2]
+        stored.append(x)
+    K, V = stored
+    f, f_dev = P.inv_freq(rotary)
+    new = api.kv_append_paged(cache, P.dev(K, dtype), P.dev(V, dtype), P.i32([3]), inv_freq=f_dev)
+    P.check_append(host, exps, cache, K, V, dtype, [3], [n], None, f, False, 0, new)
+    for x, pool in ((K, cache.k), (V, cache.v)):
+        rows = P.decode(pool.cpu().numpy()).transpose(1, 0, 2, 3).reshape(H, -1, D)[:, 3:3 + n]
+        np.testing.assert_array_equal(np.isnan(rows), np.isnan(wl.to_f64(x, dtype)[0]))
