@@ -360,7 +360,9 @@ OT_API int ot_kv_append(const ot_attn_params* p, void* K_prefix, void* V_prefix,
  *   pos * inv_freq[j]:  (u cos - v sin, u sin + v cos);  columns from R on are not turned.
  * Arithmetic in fp32, the angle, its sine and cosine in fp64 (a position of 10^6 leaves an fp32 angle two digits); one rounding at the end.
  * Q_out / K_out may be Q / K themselves (same pointer and strides); otherwise outputs must not overlap inputs.  Inputs may be
- * broadcast (a stride of 0), outputs may not (OT_ERR_INVALID_ARG).
+ * broadcast (a stride of 0) or overlap themselves; the rows of an output may not: in the order of their strides, every axis of more
+ * than one entry steps over all that the axes before it span, as in any slice or transposition of a tensor in one piece
+ * (OT_ERR_INVALID_ARG otherwise).
  * The sum of squares is held in fp32: rows with |x| above 2^60 are outside the norm's range, and with eps = 0 a row of zeros is 0 / 0.
  * Either of Q, K may be absent (q_heads / kv_heads = 0, its pointers ignored).  Infinities and NaNs stay in their own row.
  * ---------------------------------------------------------------------- */
@@ -419,8 +421,8 @@ typedef struct ot_paged_cache {
  * the capacity, and all rows from the first table entry (at or after the page of row cache_len[b]) that is no page, are
  * dropped; new_len[b] = cache_len[b] + rows stored.  A row index outside [0, n) stores a row of zeros.  Rows behind the new
  * ones keep their bytes.  Pages that receive rows must not be shared by two sequences of the call or appear
- * twice among a sequence's pages that do; K and V must not overlap the pool, and may be broadcast (a stride of 0) where the pool
- * may not (OT_ERR_INVALID_ARG).  new_len must not overlap cache_len, count or rows. */
+ * twice among a sequence's pages that do; K and V must not overlap the pool, and may be broadcast (a stride of 0) where rows of
+ * the pool may not overlap (OT_ERR_INVALID_ARG, the rule of ot_qk_norm_rope's outputs).  new_len must not overlap cache_len, count or rows. */
 typedef struct ot_append_params {
     int32_t batch, n;                   /* 1..OT_MAX_APPEND rows per sequence in K and V; batch * n < 2^31 */
     int32_t dtype;                      /* OT_F32 | OT_BF16, of K and V */
@@ -440,7 +442,8 @@ OT_API int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* c
  * the tree's keys are not in the cache yet.
  *   O[b,h,i,:] = sum_j softmax_j(scale * Q[b,h,i,:] . K[b,h/g,j,:]) V[b,h/g,j,:],  j over cache rows 0..prefix_len[b]-1 and the
  *   tree rows j with bit j of mask[b][i];  a query that sees nothing yields zeros.
- * Every input may be broadcast (a stride of 0), O may not (OT_ERR_INVALID_ARG) and must not overlap an input.
+ * Every input may be broadcast (a stride of 0); rows of O may not overlap (OT_ERR_INVALID_ARG, the rule of ot_qk_norm_rope's
+ * outputs) and must not overlap an input.
  * Cache rows from prefix_len[b] on and tree rows that no query of their sequence sees may hold anything, infinities and NaNs
  * included; tree rows that some query sees must be finite.  Mask bits from tree_keys on mean nothing.  |scale * log2(e) * Q.K| stays below 2^31.
  * prefix_len[b] is clamped to [0, max_pages * page_size] and rows of table entries that are no pages are left out (not seen

@@ -28,9 +28,21 @@ inline int sequences_per_launch(int batch, long long threads_per_sequence) {
     const long long most = 0xffffffffLL / threads_per_sequence, launches = (batch + most - 1) / most;
     return (int)((batch + launches - 1) / launches);
 }
-// Does a tensor of these sizes and strides hold the same row twice (broadcast)?  Right for what is read, a race where it is written.
-inline bool repeats(const int64_t* strides, int64_t n0, int64_t n1, int64_t n2) {
-    return (strides[0] == 0 && n0 > 1) || (strides[1] == 0 && n1 > 1) || (strides[2] == 0 && n2 > 1);
+// Can two rows of `width` elements of a tensor of these sizes and strides lie over one another?  Right for what is read, a race where
+// it is written.  Axes in the order of their strides: each steps over all that those before it span, which holds for every slice and
+// transposition of a tensor in one piece; an axis of one entry says nothing.
+inline bool overlaps(const int64_t* strides, int64_t n0, int64_t n1, int64_t n2, int64_t width) {
+    struct { int64_t stride, n; } axis[3] = {{strides[0], n0}, {strides[1], n1}, {strides[2], n2}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (axis[j].stride > axis[j + 1].stride) { const auto t = axis[j]; axis[j] = axis[j + 1]; axis[j + 1] = t; }
+    __int128 span = width;
+    for (const auto& x : axis) {
+        if (x.n <= 1) continue;
+        if (x.stride < span) return true;
+        span += (__int128)(x.n - 1) * x.stride;
+    }
+    return false;
 }
 
 // Frontier sizes F_0 = 1, F_{t+1} = min(n, k F_t) and their prefix sums

@@ -251,7 +251,8 @@ int validate_append(const ot_append_params* p, const ot_paged_cache* c) {
     if (p->interleaved != 0 && p->interleaved != 1) return OT_ERR_INVALID_ARG;
     if (p->rotary_dim < 0 || p->rotary_dim > c->head_dim) return OT_ERR_INVALID_ARG;
     if (p->rotary_dim % 16) return OT_ERR_UNSUPPORTED;
-    if (repeats(c->k_strides, c->num_pages, c->kv_heads, 1) || repeats(c->v_strides, c->num_pages, c->kv_heads, 1)) return OT_ERR_INVALID_ARG;
+    for (const int64_t* pool : {c->k_strides, c->v_strides})
+        if (overlaps(pool, c->num_pages, c->kv_heads, c->page_size, c->head_dim)) return OT_ERR_INVALID_ARG;
     if ((long long)p->batch * p->n > 0x7fffffffLL || p->n > OT_MAX_APPEND || c->kv_heads > 65535) return OT_ERR_UNSUPPORTED;
     const int vec = p->dtype == OT_BF16 ? 8 : 4;
     for (int i = 0; i < 3; ++i)

@@ -1045,7 +1045,7 @@ int validate_paged(const ot_paged_attn_params* p, const ot_paged_cache* c, bool 
     for (int t = 0; t < (p->tree_keys ? 4 : 2); ++t)
         for (int i = 0; i < 3; ++i)
             if (st4[t][i] < 0 || st4[t][i] % 8) return OT_ERR_INVALID_ARG;
-    if (repeats(p->o_strides, p->batch, p->q_heads, p->n)) return OT_ERR_INVALID_ARG;
+    if (overlaps(p->o_strides, p->batch, p->q_heads, p->n, c->head_dim)) return OT_ERR_INVALID_ARG;
     return OT_OK;
 }
 

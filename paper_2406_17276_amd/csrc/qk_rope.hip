@@ -104,7 +104,7 @@ int validate_qk(const ot_qk_params* p) {
         if ((t % 2 == 0 ? p->q_heads : p->kv_heads) == 0) continue;
         for (int i = 0; i < 3; ++i)
             if (st[t][i] < 0 || st[t][i] % vec) return OT_ERR_INVALID_ARG;
-        if (t >= 2 && repeats(st[t], p->batch, t == 2 ? p->q_heads : p->kv_heads, p->n)) return OT_ERR_INVALID_ARG;
+        if (t >= 2 && overlaps(st[t], p->batch, t == 2 ? p->q_heads : p->kv_heads, p->n, p->head_dim)) return OT_ERR_INVALID_ARG;
     }
     return OT_OK;
 }
