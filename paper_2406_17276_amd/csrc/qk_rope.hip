@@ -139,14 +139,14 @@ int ot_qk_norm_rope(const ot_qk_params* p, const void* Q, const void* K, const v
     // two passes of rows per workgroup (four: 149 us, not 130, at 15009 tokens x 40 heads in fp32)
     a.tokens = std::min(kMaxTokens, std::max(1, 2 * rpp / a.heads));
     a.share = a.heads;
-    if ((a.all_tokens + a.tokens - 1) / a.tokens < 512) {      // few tokens: a token each, heads over several workgroups
+    if (((long long)a.all_tokens + a.tokens - 1) / a.tokens < 512) {      // few tokens: a token each, heads over several workgroups
         a.tokens = 1;
         if (a.all_tokens < 512) a.share = std::min(a.heads, rpp);
     }
     a.inv_share = a.share > 1 ? (unsigned)((0x100000000ull + a.share - 1) / a.share) : 0;
     const unsigned shares = (unsigned)((a.heads + a.share - 1) / a.share);
     // a grid holds fewer than 2^32 threads: more tokens go in several launches
-    const int groups = sequences_per_launch((a.all_tokens + a.tokens - 1) / a.tokens, (long long)shares * kThreads);
+    const int groups = sequences_per_launch((int)(((long long)a.all_tokens + a.tokens - 1) / a.tokens), (long long)shares * kThreads);
     hipStream_t s = (hipStream_t)hip_stream;
     for (long long base = 0; base < a.all_tokens; base += (long long)groups * a.tokens) {
         a.base = (int)base;
