@@ -470,6 +470,11 @@ const at::Tensor* heads4(PyObject* o, const OnDevice& on, const char* name) {
     if (t.stride(3) != 1) fail(PyExc_ValueError, "last dimension of %s must be contiguous", name);
     return &t;
 }
+// a size as the C structs have it: one that 32 bits do not hold (a broadcast axis may be as long as it likes) is no size of these calls
+int32_t size32(int64_t n, const char* what) {
+    if (n != (int32_t)n) fail(PyExc_ValueError, "%s must fit 32 bits", what);
+    return (int32_t)n;
+}
 bool same_shape(const at::Tensor& x, const at::Tensor& y) { return x.sizes() == y.sizes(); }
 
 // (Q | None, K | None, q_weight | None, k_weight | None, inv_freq | None, first, offset | None, shift, eps, interleaved,
@@ -483,12 +488,11 @@ PyObject* qk_norm_rope(PyObject* const* a, Py_ssize_t na) {
     if (Q && K && (Q->size(0) != K->size(0) || Q->size(2) != K->size(2) || Q->size(3) != K->size(3) || Q->scalar_type() != K->scalar_type()))
         fail(PyExc_ValueError, "Q and K must agree in batch, tokens, head_dim and dtype");
     ot_qk_params p{};
-    p.batch = (int32_t)x.size(0); p.n = (int32_t)x.size(2); p.head_dim = (int32_t)x.size(3);
-    if (p.batch != x.size(0) || p.n != x.size(2)) fail(PyExc_ValueError, "batch and tokens must fit 32 bits");
-    p.q_heads = Q ? (int32_t)Q->size(1) : 0; p.kv_heads = K ? (int32_t)K->size(1) : 0;
+    p.batch = size32(x.size(0), "batch"); p.n = size32(x.size(2), "tokens"); p.head_dim = size32(x.size(3), "head_dim");
+    p.q_heads = Q ? size32(Q->size(1), "heads") : 0; p.kv_heads = K ? size32(K->size(1), "heads") : 0;
     p.dtype = dtype_code(x);
     const at::Tensor* inv = array(a[4], on, at::kDouble, {-1}, "inv_freq", true);
-    p.rotary_dim = inv ? (int32_t)(2 * inv->numel()) : 0;
+    p.rotary_dim = inv ? size32(2 * inv->numel(), "rotary_dim") : 0;
     p.shift = as_int(a[7]); p.eps = (float)as_double(a[8]); p.interleaved = as_int(a[9]);
     const at::Tensor* qw = array(a[2], on, x.scalar_type(), {p.head_dim}, "q_weight", true);
     const at::Tensor* kw = array(a[3], on, x.scalar_type(), {p.head_dim}, "k_weight", true);
@@ -518,8 +522,8 @@ ot_paged_cache paged_cache(PyObject* const* a, const OnDevice& on, int64_t batch
     const at::Tensor &k = *heads4(a[0], on, "cache.k"), &v = *heads4(a[1], on, "cache.v");
     if (!same_shape(k, v) || k.scalar_type() != v.scalar_type()) fail(PyExc_ValueError, "cache.k and cache.v must agree in shape and dtype");
     ot_paged_cache c{};
-    c.num_pages = (int32_t)k.size(0); c.kv_heads = (int32_t)k.size(1); c.page_size = (int32_t)k.size(2); c.head_dim = (int32_t)k.size(3);
-    if (c.num_pages != k.size(0)) fail(PyExc_ValueError, "pages must fit 32 bits");
+    c.num_pages = size32(k.size(0), "pages"); c.kv_heads = size32(k.size(1), "heads of the cache");
+    c.page_size = size32(k.size(2), "rows of a page"); c.head_dim = size32(k.size(3), "head_dim");
     const bool eight = k.scalar_type() == at::kByte || k.scalar_type() == at::kFloat8_e4m3fn;
     if (!eight && k.scalar_type() != at::kBFloat16) fail(PyExc_TypeError, "pages are bfloat16, or uint8 / float8_e4m3fn");
     c.dtype = eight ? OT_E4M3 : OT_BF16;
@@ -530,7 +534,7 @@ ot_paged_cache paged_cache(PyObject* const* a, const OnDevice& on, int64_t batch
         c.v_exp = (uint8_t*)ptr(array(a[3], on, at::kByte, {k.size(0), k.size(1)}, "cache.v_exp", false));
     }
     const at::Tensor* table = array(a[4], on, at::kInt, {batch, -1}, "cache.table", false);
-    c.max_pages = (int32_t)table->size(1);
+    c.max_pages = size32(table->size(1), "pages of a sequence");
     c.page_table = (const int32_t*)ptr(table);
     return c;
 }
@@ -546,8 +550,7 @@ PyObject* kv_append_paged(PyObject* const* a, Py_ssize_t na) {
     const ot_paged_cache c = paged_cache(a + 2, on, K.size(0));
     if (K.size(1) != c.kv_heads || K.size(3) != c.head_dim) fail(PyExc_ValueError, "K and the cache must agree in heads and head_dim");
     ot_append_params p{};
-    p.batch = (int32_t)K.size(0); p.n = (int32_t)K.size(2);
-    if (p.batch != K.size(0) || p.n != K.size(2)) fail(PyExc_ValueError, "batch and rows must fit 32 bits");
+    p.batch = size32(K.size(0), "batch"); p.n = size32(K.size(2), "rows");
     p.dtype = dtype_code(K);
     strides_of(K, p.k_strides); strides_of(V, p.v_strides);
     const at::Tensor* len = array(a[7], on, at::kInt, {p.batch}, "cache_len", false);
@@ -555,7 +558,7 @@ PyObject* kv_append_paged(PyObject* const* a, Py_ssize_t na) {
     const at::Tensor* rows = array(a[9], on, at::kInt, {p.batch, p.n}, "rows", true);
     p.count_shift = as_int(a[10]);
     const at::Tensor* inv = array(a[11], on, at::kDouble, {-1}, "inv_freq", true);
-    p.rotary_dim = inv ? (int32_t)(2 * inv->numel()) : 0;
+    p.rotary_dim = inv ? size32(2 * inv->numel(), "rotary_dim") : 0;
     p.shift = as_int(a[12]); p.interleaved = as_int(a[13]);
     at::Tensor own;
     const at::Tensor* nl = array(a[14], on, at::kInt, {p.batch}, "new_len", true);
@@ -583,8 +586,8 @@ PyObject* attention_paged(PyObject* const* a, Py_ssize_t na) {
                Kt->size(1) != c.kv_heads || Kt->size(3) != c.head_dim))
         fail(PyExc_ValueError, "K_tree and V_tree must be bfloat16 [B, Hkv, keys, D]");
     ot_paged_attn_params p{};
-    p.batch = (int32_t)Q.size(0); p.q_heads = (int32_t)Q.size(1); p.n = (int32_t)Q.size(2);
-    p.tree_keys = Kt ? (int32_t)Kt->size(2) : 0;
+    p.batch = size32(Q.size(0), "batch"); p.q_heads = size32(Q.size(1), "heads"); p.n = size32(Q.size(2), "queries");
+    p.tree_keys = Kt ? size32(Kt->size(2), "tree keys") : 0;
     p.softmax_scale = (float)as_double(a[12]);
     const at::Tensor* len = array(a[8], on, at::kInt, {p.batch}, "prefix_len", false);
     const at::Tensor* mask = Kt ? array(a[9], on, at::kLong, {p.batch, p.n, OT_MASK_WORDS(p.tree_keys)}, "mask", false) : nullptr;

@@ -105,3 +105,28 @@ def test_signalling_nans_hide_no_value(dtype, D, ps, rotary):
     for x, pool in ((K, cache.k), (V, cache.v)):
         rows = P.decode(pool.cpu().numpy()).transpose(1, 0, 2, 3).reshape(H, -1, D)[:, 3:3 + n]
         np.testing.assert_array_equal(np.isnan(rows), np.isnan(wl.to_f64(x, dtype)[0]))
+
+
+def test_sizes_that_32_bits_do_not_hold_are_refused():
+    """An axis of 2^32 + 3 rows, broadcast from one, is not one of 3."""
+    import torch
+    from paper_2406_17276_amd import api
+    cache = api.alloc_paged_cache(4, 2, 16, 64, 1, 2)
+    new = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+    far, q, mask = (1 << 32) + 3, new(1, 2, 3, 64), torch.zeros(1, 3, 1, dtype=torch.int64, device="cuda")
+    ws = api.paged_attn_workspace(q, cache)
+    long = new(1, 2, 1, 64).expand(-1, -1, far, -1)
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(q, cache, P.i32([0]), long, long, mask, workspace=ws)
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(long, cache, P.i32([0]), out=long, workspace=ws)
+    many = new(1, 1, 3, 64).expand(-1, (1 << 32) + 2, -1, -1)
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(many, cache, P.i32([0]), out=many, workspace=ws)
+    with pytest.raises(ValueError):
+        api.qk_norm_rope(many, None, P.i32([0]), q_out=many)
+    heads = cache.k[:, :1].expand(-1, (1 << 32) + 2, -1, -1)
+    with pytest.raises(ValueError):
+        api.tree_verify_attention_paged(q, api.PagedCache(heads, heads, cache.table, cache.k_exp, cache.v_exp), P.i32([0]), workspace=ws)
+    with pytest.raises(ValueError):
+        api.kv_append_paged(cache, long, long, P.i32([0]))
