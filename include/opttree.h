@@ -359,7 +359,7 @@ OT_API int ot_kv_append(const ot_attn_params* p, void* K_prefix, void* V_prefix,
  *   the pair (y_j, y_{j+R/2}), R = rotary_dim, or with `interleaved` (y_2j, y_2j+1), j < R/2, is turned by the angle
  *   pos * inv_freq[j]:  (u cos - v sin, u sin + v cos);  columns from R on are not turned.
  * Arithmetic in fp32, the angle, its sine and cosine in fp64 (a position of 10^6 leaves an fp32 angle two digits); one rounding at the end.
- * Q_out / K_out may be Q / K themselves (same pointer and strides); otherwise outputs must not overlap inputs.  Inputs may be
+ * Q_out / K_out may be Q / K themselves (same pointer and strides); otherwise outputs must not overlap inputs, nor each other.  Inputs may be
  * broadcast (a stride of 0) or overlap themselves; the rows of an output may not: in the order of their strides, every axis of more
  * than one entry steps over all that the axes before it span, as in any slice or transposition of a tensor in one piece
  * (OT_ERR_INVALID_ARG otherwise).
@@ -422,7 +422,8 @@ typedef struct ot_paged_cache {
  * dropped; new_len[b] = cache_len[b] + rows stored.  A row index outside [0, n) stores a row of zeros.  Rows behind the new
  * ones keep their bytes.  Pages that receive rows must not be shared by two sequences of the call or appear
  * twice among a sequence's pages that do; K and V must not overlap the pool, and may be broadcast (a stride of 0) where rows of
- * the pool may not overlap (OT_ERR_INVALID_ARG, the rule of ot_qk_norm_rope's outputs).  new_len must not overlap cache_len, count or rows. */
+ * the pool may not overlap (OT_ERR_INVALID_ARG, the rule of ot_qk_norm_rope's outputs).  new_len must not overlap cache_len, count or rows;
+ * keys and values must not share rows or exponents (equal pointers: OT_ERR_INVALID_ARG; a cache that is only read may). */
 typedef struct ot_append_params {
     int32_t batch, n;                   /* 1..OT_MAX_APPEND rows per sequence in K and V; batch * n < 2^31 */
     int32_t dtype;                      /* OT_F32 | OT_BF16, of K and V */

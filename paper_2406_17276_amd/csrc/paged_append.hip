@@ -300,6 +300,8 @@ int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* cache, c
     // workgroups still read these while new_len is written
     const size_t nb = (size_t)p->batch * 4;
     if (overlap(new_len, nb, cache_len, nb) || overlap(new_len, nb, count, nb) || overlap(new_len, nb, rows, nb * p->n)) return OT_ERR_INVALID_ARG;
+    // keys and values of one row at one address, or their exponents
+    if (cache->k_pages == cache->v_pages || (cache->dtype == OT_E4M3 && cache->k_exp == cache->v_exp)) return OT_ERR_INVALID_ARG;
     AppendArgs a;
     a.K = K; a.V = V; a.kp = (unsigned char*)cache->k_pages; a.vp = (unsigned char*)cache->v_pages;
     a.k_exp = cache->k_exp; a.v_exp = cache->v_exp;

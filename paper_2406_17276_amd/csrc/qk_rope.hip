@@ -123,6 +123,7 @@ int ot_qk_norm_rope(const ot_qk_params* p, const void* Q, const void* K, const v
     if (st != OT_OK) return st;
     if ((p->q_heads && (!Q || !Q_out)) || (p->kv_heads && (!K || !K_out)) || !first) return OT_ERR_INVALID_ARG;
     if (p->rotary_dim && !inv_freq) return OT_ERR_INVALID_ARG;
+    if (p->q_heads && p->kv_heads && Q_out == K_out) return OT_ERR_INVALID_ARG;
     const void* v[6] = {p->q_heads ? Q : nullptr, p->q_heads ? Q_out : nullptr, p->q_heads ? q_weight : nullptr,
                         p->kv_heads ? K : nullptr, p->kv_heads ? K_out : nullptr, p->kv_heads ? k_weight : nullptr};
     for (const void* x : v)

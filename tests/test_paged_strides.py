@@ -54,6 +54,22 @@ def test_overlapping_pages_are_read_but_not_written(dtype, name, pool):
     L = api.lib()
     if pool[2] == 72 and dtype == api.OT_E4M3:
         pool = (2048, 1024, 80)
-    c = _cache(dtype=dtype, **{name: s3(*pool)})
+    c = _cache(dtype=dtype, v_pages=0x100000, v_exp=0x2000, **{name: s3(*pool)})
     assert L.ot_kv_append_paged(C.byref(_ap()), C.byref(c), F, F, F, F, F, F, FAR, None) == -1
     assert L.ot_paged_attn_workspace_bytes(C.byref(_pp()), C.byref(c)) > 0
+
+
+def test_two_outputs_at_one_address_are_not_written():
+    """Pointers that no GPU has: a call that is not refused fails at its launch (no GPU) with another status."""
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("would launch if it were not refused")
+    L = api.lib()
+    apart = dict(v_pages=0x100000, v_exp=0x2000)
+    call = lambda c: L.ot_kv_append_paged(C.byref(_ap()), C.byref(c), F, F, F, F, F, F, FAR, None)
+    assert call(_cache(**apart)) == -4                                      # nothing wrong with it but the missing GPU
+    assert call(_cache(v_exp=0x2000)) == -1 and call(_cache(v_pages=0x100000)) == -1
+    assert call(_cache(**{**apart, "dtype": api.OT_BF16, "v_exp": 0x1000})) == -4        # exponents that are not used
+    qk = lambda q, k, **kw: L.ot_qk_norm_rope(C.byref(_qk(**kw)), F, F, F, F, F, F, F, C.c_void_p(q), C.c_void_p(k), None)
+    assert qk(0x10000, 0x10000) == -1 and qk(0x10000, 0x20000) == -4
+    assert qk(0x10000, 0x10000, kv_heads=0) == -4 and qk(0x10000, 0x10000, q_heads=0) == -4
