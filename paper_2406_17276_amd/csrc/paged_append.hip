@@ -1,7 +1,7 @@
 // Rows join a paged K/V cache, keys turned by their position on the way (opttree.h: ot_kv_append_paged).
 //
 // What bounds it: rows are read once (f32 or bf16) and written once (bf16, or bytes); single tokens and branches are launch
-// latency and a chain length -> page -> older exponent -> store.
+// latency and a chain length -> page -> older exponent -> store.  Table entries are read anew for every page (kKnownPages).
 //
 // The unit of work is a page that receives rows, because an 8-bit page has one exponent per head: its new rows' largest
 // magnitude has to be known before the first of them is stored.  A workgroup takes one such page of one sequence and a share
@@ -33,6 +33,7 @@ struct AppendArgs {
     int num_pages, max_pages, ps_log2;
     int shift, count_shift;
     int base;                            // first sequence of this launch
+    int lengths_known;                   // new_len holds what this call stores
     long long ks[3], vs[3], kps[3], vps[3];
 };
 
@@ -68,6 +69,42 @@ __device__ __forceinline__ unsigned pack_e4m3(float x, float y, float z, float w
 }
 __device__ __forceinline__ float saturate(float x) { return x > 448.f ? 448.f : (x < -448.f ? -448.f : x); }
 
+// Rows of sequence b before the call, and those asked for, less what the capacity drops
+struct Span {
+    int len, cnt;
+};
+__device__ __forceinline__ Span span_of(const AppendArgs& a, int b) {
+    const int cap = a.max_pages << a.ps_log2, len = min(max(a.cache_len[b], 0), cap);
+    const long long want = a.count ? (long long)a.count[b] + a.count_shift : (long long)a.n;
+    return Span{len, (int)min((long long)min(a.n, cap - len), max(want, 0LL))};
+}
+// new_len of sequence b, by a workgroup: rows are stored up to the first table entry that is no page
+template <int NT>
+__device__ __forceinline__ void write_new_len(const AppendArgs& a, int b, const Span& x) {
+    __shared__ int s_stop[NT / 64];
+    const int32_t* const table = a.table + (long long)b * a.max_pages;
+    const int tid = threadIdx.x, p_first = x.len >> a.ps_log2, p_last = (x.len + x.cnt - 1) >> a.ps_log2;
+    int stop = p_last + 1;
+#pragma unroll 4
+    for (int p = p_first + tid; p <= p_last; p += NT)
+        if ((unsigned)table[p] >= (unsigned)a.num_pages) stop = min(stop, p);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) stop = min(stop, __shfl_xor(stop, o));
+    if ((tid & 63) == 0) s_stop[tid >> 6] = stop;
+    __syncthreads();
+    if (tid == 0) {
+        for (int w = 1; w < NT / 64; ++w) stop = min(stop, s_stop[w]);
+        a.new_len[b] = x.cnt == 0 ? x.len : (stop > p_last ? x.len + x.cnt : max(x.len, stop << a.ps_log2));
+    }
+}
+// Ahead of an append of many pages (kKnownPages)
+__global__ __launch_bounds__(1024) void paged_new_len_kernel(const AppendArgs a) { write_new_len<1024>(a, blockIdx.x, span_of(a, blockIdx.x)); }
+// A workgroup looks at its sequence's table entries from the first new page to its own, since rows behind one that is no page are
+// dropped: P^2 / 2 reads for P pages, nothing beside the rows of a thousand pages and more than them beyond.  With more pages than this
+// a launch ahead finds the new lengths once.  us without it and with it, pages of 16, 2 heads of 64: 7.0 and 8.1 for 1024 pages, 9.6 and
+// 9.7 for 1536, 24.0 and 16.4 for 4096, 1875 and 252 for 65536; 8 heads of 128: 22.4 and 20.6, 32.0 and 27.3, 140 and 83 for 4096.
+constexpr int kKnownPages = 1536;
+
 template <int DT, bool KV8, int D, int NT, bool TOGETHER>
 __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a) {
     constexpr int LPR = D / 16;                // lanes per row
@@ -80,34 +117,20 @@ __global__ __launch_bounds__(NT) void kv_append_paged_kernel(const AppendArgs a)
     const int tid = threadIdx.x, wave = tid >> 6;
     const int ht = tid % HALF, t = ht % LPR, r_first = ht / LPR;
     const int b = a.base + blockIdx.z;
-    const int ps = 1 << a.ps_log2, cap = a.max_pages << a.ps_log2;
-    const int len = min(max(a.cache_len[b], 0), cap);
-    const long long want = a.count ? (long long)a.count[b] + a.count_shift : (long long)a.n;
-    const int cnt = (int)min((long long)min(a.n, cap - len), max(want, 0LL));
+    const int ps = 1 << a.ps_log2;
+    Span x = span_of(a, b);
+    if (a.lengths_known) x.cnt = a.new_len[b] - x.len;
+    const int len = x.len, cnt = x.cnt;
     const int p_first = len >> a.ps_log2, p_last = (len + cnt - 1) >> a.ps_log2;      // (cnt = 0: p_last <= p_first)
     const int page_slot = p_first + blockIdx.x;
     const int32_t* const table = a.table + (long long)b * a.max_pages;
-    const bool first_wg = blockIdx.x == 0 && blockIdx.y == 0;
-    if (first_wg) {
-        // rows stored: up to the first table entry that is no page
-        int stop = p_last + 1;
-        for (int p = p_first + tid; p <= p_last; p += NT) {
-            if ((unsigned)table[p] >= (unsigned)a.num_pages) { stop = p; break; }
-        }
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) stop = min(stop, __shfl_xor(stop, o));
-        __shared__ int s_stop[NT / 64];
-        if ((tid & 63) == 0) s_stop[wave] = stop;
-        __syncthreads();
-        if (tid == 0) {
-            for (int w = 1; w < NT / 64; ++w) stop = min(stop, s_stop[w]);
-            a.new_len[b] = cnt == 0 ? len : (stop > p_last ? len + cnt : max(len, stop << a.ps_log2));
-        }
-    }
+    if (!a.lengths_known && blockIdx.x == 0 && blockIdx.y == 0) write_new_len<NT>(a, b, x);
     if (cnt == 0 || page_slot > p_last) return;
-    bool bad = false;
-    for (int p = p_first + tid; p <= page_slot; p += NT) bad |= (unsigned)table[p] >= (unsigned)a.num_pages;
-    if (__syncthreads_or(bad)) return;
+    if (!a.lengths_known) {
+        bool bad = false;
+        for (int p = p_first + tid; p <= page_slot; p += NT) bad |= (unsigned)table[p] >= (unsigned)a.num_pages;
+        if (__syncthreads_or(bad)) return;
+    }
     const int page = table[page_slot];
     const int row0 = max(0, len - (page_slot << a.ps_log2)), row1 = min(ps, len + cnt - (page_slot << a.ps_log2));
     const int j0 = (page_slot << a.ps_log2) - len;                 // list position of the page's row 0
@@ -323,6 +346,11 @@ int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* cache, c
     const unsigned shares = (unsigned)((a.heads + a.share - 1) / a.share);
     const size_t lds = (size_t)ps * (p->rotary_dim / 2) * sizeof(float2);
     hipStream_t s = (hipStream_t)hip_stream;
+    a.lengths_known = pages > kKnownPages;
+    if (a.lengths_known) {                                         // (batch * n < 2^31: fewer than 2^15 sequences)
+        hipLaunchKernelGGL(paged_new_len_kernel, dim3((unsigned)p->batch), dim3(1024), 0, s, a);
+        OT_HIP_CHECK(hipGetLastError());
+    }
     const int per = std::min(65535, sequences_per_launch(p->batch, pages * shares * 1024LL));
     for (int base = 0; base < p->batch; base += per) {
         a.base = base;

@@ -130,3 +130,63 @@ def test_sizes_that_32_bits_do_not_hold_are_refused():
         api.tree_verify_attention_paged(q, api.PagedCache(heads, heads, cache.table, cache.k_exp, cache.v_exp), P.i32([0]), workspace=ws)
     with pytest.raises(ValueError):
         api.kv_append_paged(cache, long, long, P.i32([0]))
+
+
+@pytest.mark.parametrize("eight", [True, False])
+def test_an_append_of_very_many_pages_equals_its_pieces(eight):
+    """Sequences of up to 80000 pages in one call and in calls of 2000 pages each; one of them meets a table entry that is no page, one
+    its capacity, one is nearly empty."""
+    import torch
+    from paper_2406_17276_amd import api
+    torch.manual_seed(2)
+    H, D, ps, B, most = 1, 64, 16, 4, 80000
+    lens, n = [0, 5, 16 * 70000, 3], 16 * 79000
+    count = [n, n, n, 7]
+    caches = [api.alloc_paged_cache(B * most, H, ps, D, B, most, eight_bit=eight) for _ in range(2)]
+    table = torch.randperm(B * most, device="cuda", dtype=torch.int32).view(B, most)
+    table[1, 41234], table[1, 60000] = -1, B * most
+    for c in caches:
+        c.k.zero_(), c.v.zero_(), c.table.copy_(table)
+    K, V = (torch.randn(1, H, n, D, device="cuda").to(torch.bfloat16).expand(B, -1, -1, -1) for _ in range(2))
+    new = api.kv_append_paged(caches[0], K, V, P.i32(lens), count=P.i32(count))
+    want = [n, 16 * 41234, 16 * 80000, 10]
+    assert new.tolist() == want
+    at = P.i32(lens)
+    step = 16 * 2000
+    for j in range(0, n, step):
+        for b in range(B):
+            skew = 11 if b == 1 else 0                                   # row 5 + 11 begins a page: later pieces begin with theirs
+            lo, hi = (j + skew if j else 0), min(n, j + step + skew)
+            m = max(0, min(hi, count[b]) - lo)
+            if m:
+                one = api.PagedCache(caches[1].k, caches[1].v, table[b:b + 1], caches[1].k_exp, caches[1].v_exp)
+                at[b:b + 1] = api.kv_append_paged(one, K[:1, :, lo:lo + m], V[:1, :, lo:lo + m], at[b:b + 1].clone())
+                if int(at[b]) == want[b]:
+                    count[b] = 0                                         # what comes after a missing page is dropped, not moved up
+    assert at.tolist() == want
+    assert torch.equal(caches[0].k, caches[1].k) and torch.equal(caches[0].v, caches[1].v)
+    if eight:
+        assert torch.equal(caches[0].k_exp, caches[1].k_exp) and torch.equal(caches[0].v_exp, caches[1].v_exp)
+
+
+def test_a_long_append_costs_what_its_pieces_cost():
+    """1048576 rows into pages of 16 at once, and 65536 at a time: a cost per row that grows with the length would show as 16 times."""
+    import torch
+    from paper_2406_17276_amd import api
+    H, D, ps, n, parts = 2, 64, 16, 1 << 20, 16
+    cache = api.alloc_paged_cache(n // ps, H, ps, D, 1, n // ps, eight_bit=False)
+    cache.table.copy_(torch.randperm(n // ps, device="cuda", dtype=torch.int32)[None])
+    K = torch.randn(1, H, n, D, device="cuda").to(torch.bfloat16)
+    at = [P.i32([i * (n // parts)]) for i in range(parts)]
+    rows = [K[:, :, i * (n // parts):(i + 1) * (n // parts)] for i in range(parts)]
+    calls = (lambda: api.kv_append_paged(cache, K, K, at[0]), lambda: [api.kv_append_paged(cache, r, r, a) for r, a in zip(rows, at)])
+
+    def best(f):
+        times = []
+        for _ in range(7):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record(), f(), e[1].record()
+            torch.cuda.synchronize()
+            times.append(e[0].elapsed_time(e[1]))
+        return min(times)
+    assert best(calls[0]) < 2 * best(calls[1])
