@@ -363,11 +363,12 @@ OT_API int ot_kv_append(const ot_attn_params* p, void* K_prefix, void* V_prefix,
  * broadcast (a stride of 0) or overlap themselves; the rows of an output may not: in the order of their strides, every axis of more
  * than one entry steps over all that the axes before it span, as in any slice or transposition of a tensor in one piece
  * (OT_ERR_INVALID_ARG otherwise).
- * The sum of squares is held in fp32: rows with |x| above 2^60 are outside the norm's range, and with eps = 0 a row of zeros is 0 / 0.
+ * The sum of squares is held in fp32: rows with |x| above 2^60 are outside the norm's range, so are rows with no |x| above 2^-56 where
+ * eps is below 2^-100, and with eps = 0 a row of zeros is 0 / 0.
  * Either of Q, K may be absent (q_heads / kv_heads = 0, its pointers ignored).  Infinities and NaNs stay in their own row.
  * ---------------------------------------------------------------------- */
 typedef struct ot_qk_params {
-    int32_t batch, q_heads, kv_heads;   /* heads >= 0, not both 0 */
+    int32_t batch, q_heads, kv_heads;   /* heads >= 0, not both 0, at most 65535 together */
     int32_t head_dim;                   /* 64 or 128 */
     int32_t n;                          /* tokens per sequence, >= 1; batch * n < 2^31 */
     int32_t dtype;                      /* OT_F32 | OT_BF16, of Q, K, the weights and the outputs */
@@ -399,12 +400,12 @@ OT_API int ot_qk_norm_rope(const ot_qk_params* p, const void* Q, const void* K,
  * ---------------------------------------------------------------------- */
 typedef struct ot_paged_cache {
     int32_t num_pages, page_size;       /* page_size: 16, 32, 64, 128 or 256 */
-    int32_t kv_heads, head_dim;         /* head_dim 64 or 128 */
+    int32_t kv_heads, head_dim;         /* head_dim 64 or 128; num_pages * kv_heads < 2^31 */
     int32_t dtype;                      /* OT_BF16 | OT_E4M3 */
     int32_t max_pages;                  /* entries per sequence in page_table; max_pages * page_size < 2^30 */
-    int64_t k_strides[3], v_strides[3]; /* page, head, row; elements */
+    int64_t k_strides[3], v_strides[3]; /* page, head, row; elements; pages less than 2^36 bytes apart, rows head_dim to 2^22 elements */
     void *k_pages, *v_pages;            /* device */
-    uint8_t *k_exp, *v_exp;             /* device [num_pages][kv_heads], 4-byte aligned (read in aligned words of 4), OT_E4M3 only */
+    uint8_t *k_exp, *v_exp;             /* device [num_pages][kv_heads], 4-byte aligned and read in whole words of 4, the last one too; OT_E4M3 only */
     const int32_t* page_table;          /* device [batch][max_pages] */
 } ot_paged_cache;
 
@@ -413,10 +414,11 @@ typedef struct ot_paged_cache {
  * (as in ot_qk_norm_rope); the stored value is rounded once, from fp32.
  *   prompt or generated token: count = NULL (all n rows) or the lengths of padded prompts, rows = NULL
  *   accepted branch:           count = accept_len, count_shift = -1, rows = accept_node (ot_verify_greedy / _sample)
+ * At most 65535 KV heads.
  * OT_E4M3: the exponent of a page and head becomes the smallest with which no new row of this call in it exceeds 448; if the page
  * holds older rows of the sequence (those before cache_len[b]) it does not fall below what it was, and where it rises
  * the older rows are rounded again at the new one.  Infinities are stored as +-448 at the exponent of the finite values,
- * NaNs as NaN.
+ * NaNs, signalling ones too, as NaN: neither has a part in the exponent.
  * cache_len[b] is clamped to [0, capacity], capacity = max_pages * page_size; count[b] + count_shift to [0, n].  Rows beyond
  * the capacity, and all rows from the first table entry (at or after the page of row cache_len[b]) that is no page, are
  * dropped; new_len[b] = cache_len[b] + rows stored.  A row index outside [0, n) stores a row of zeros.  Rows behind the new
@@ -446,7 +448,11 @@ OT_API int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* c
  * Every input may be broadcast (a stride of 0); rows of O may not overlap (OT_ERR_INVALID_ARG, the rule of ot_qk_norm_rope's
  * outputs) and must not overlap an input.
  * Cache rows from prefix_len[b] on and tree rows that no query of their sequence sees may hold anything, infinities and NaNs
- * included; tree rows that some query sees must be finite.  Mask bits from tree_keys on mean nothing.  |scale * log2(e) * Q.K| stays below 2^31.
+ * included; cache rows before it and tree rows that some query sees must be finite.  Mask bits from tree_keys on mean nothing.
+ * |scale * log2(e) * Q.K| stays below 2^31.
+ * Scores, softmax and sums are held in fp32; the weights are rounded to bf16, the type in which the matrix cores multiply them by V (so they
+ * are in ot_tree_verify_attention), and divided by the sum of the rounded ones.  Beside the rounding of O that is an error of about
+ * 2^-8 sum w |v - O| at most.
  * prefix_len[b] is clamped to [0, max_pages * page_size] and rows of table entries that are no pages are left out (not seen
  * by any query); both are reported in the status word of the workspace (OT_ATTN_STATUS_PREFIX_CLAMPED,
  * OT_ATTN_STATUS_BAD_PAGE at OT_ATTN_STATUS_OFFSET; api: attn_status).
@@ -456,7 +462,7 @@ OT_API int ot_kv_append_paged(const ot_append_params* p, const ot_paged_cache* c
 #define OT_PAGED_SYNC_BYTES 65536
 #define OT_ATTN_STATUS_BAD_PAGE 2u
 typedef struct ot_paged_attn_params {
-    int32_t batch, q_heads;             /* q_heads % cache.kv_heads == 0 */
+    int32_t batch, q_heads;             /* q_heads % cache.kv_heads == 0; batch * q_heads <= 65535 */
     int32_t n;                          /* query rows, 1..OT_MAX_NODES */
     int32_t tree_keys;                  /* rows of K_tree / V_tree, 0..OT_MAX_TREE_KEYS; 0: no tree (K_tree, V_tree, mask ignored) */
     float   softmax_scale;              /* 0 => 1/sqrt(head_dim) */

@@ -7,7 +7,8 @@
 // a row block to finish merges them (tickets).
 //
 // Ranges are decided on the device, from the lengths as they are (find_job): a page table gives every sequence room for
-// the longest context, so the host's bound on a length says little, and lengths in a serving batch differ.
+// the longest context, so the host's bound on a length says little, and lengths in a serving batch differ.  Batches whose (sequence, KV
+// head, row block) triples fill the card by themselves are not cut, whatever their lengths (plan_paged).
 #include <math.h>
 
 #include <algorithm>
@@ -113,7 +114,7 @@ struct Job {
 // sequence: S ranges take T / S tiles and S joins of `apart` tiles each, which is least there.  Each sequence takes
 // ceil(tiles / share) ranges of equal length.  Lane j holds sequences j, j + 64, ...
 // Workgroups go to XCD wg % 8 in order; the row blocks of a KV head and range, which read the same rows, take consecutive
-// places on one XCD, whose L2 they share (16 x 8 KV heads x 4 row blocks over 8192 keys: 535 us, not 545).
+// places on one XCD, whose L2 they share (16 x 8 KV heads x 4 row blocks over 8192 keys: 322 MB fetched, not 1179; 535 us, not 545).
 __device__ __forceinline__ Job find_job(const Lead& a, unsigned int* sync, int wg) {
     const int lane = threadIdx.x & 63, cap = a.max_pages << a.ps_log2;
     const int units = a.kv_heads * a.row_blocks, place = wg >> 3, group = place / a.row_blocks;
@@ -392,7 +393,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs a) {
 // were not there and gained nothing (4 x 100000 keys: 172 us one block ahead, 177 two).  Pages are multiples of sixteen
 // rows, so a block's page numbers and exponents are two scalars each, known a block earlier.  The streams' results meet in
 // LDS at the end.
-// Measured: 8 KV heads x 8 queries over 4 x 100000 keys in 8 bits (820 MB) 138 to 148 us, 5.5 to 5.9 TB/s; 8 KV heads x 4 over 1500 keys
+// Measured: 8 KV heads x 8 queries over 4 x 100000 keys in 8 bits (820 MB) 133 to 148 us, 5.5 to 6.2 TB/s; 8 KV heads x 4 over 1500 keys
 // 10 us, a chain of eight trips to memory: length, page, exponents and rows, partial, ticket, partials.
 // ---------------------------------------------------------------------------
 template <int D, bool KV8, int QW>
@@ -715,7 +716,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 //   K [64][D]: 16-byte piece c of row r at c ^ (r mod D/8);  V [64][D]: 32-byte segment g of row r at g ^ v_swizzle(r)
 // 256 rows take eight wavefronts, one workgroup to a compute unit; up to 128 rows four, two workgroups to a unit, which drift
 // apart by themselves.
-// Measured: 16 x 8 KV heads x 1024 queries over 8192 keys in 8 bits (550 GFLOP) 535 to 575 us, 0.96 to 1.03 PFLOP/s, where a large bf16
+// Measured: 16 x 8 KV heads x 1024 queries over 8192 keys in 8 bits (550 GFLOP) 541 to 575 us, 0.96 to 1.02 PFLOP/s, where a large bf16
 // matrix product of the library reaches 1.23; 16 x 8 x 480 over 4096 +-25 % 157 to 165 us (the longest sequence decides).
 // ---------------------------------------------------------------------------
 template <int D, bool KV8, int NW>
@@ -1017,13 +1018,19 @@ PagedPlan plan_paged(const ot_paged_attn_params& p, const ot_paged_cache& c) {
     pl.slot_rows = std::min(R, pl.rows);
     const long long all = (long long)p.batch * pl.units;
     const int resident = pl.rows <= 128 ? 512 : 256;           // workgroups that the card holds
+    // As many triples as the card holds, or more than 256 sequences, stay in one piece each: cutting 16 x 8 KV heads x 480 rows over 4096
+    // keys +-25 % into twice as many jobs took 199 us instead of 160, for the second round of workgroups.  The price is a batch that one
+    // long context rules: 64 x 8 KV heads x 8 queries, 63 contexts of 1000 keys and one of 100000, 955 us (62 and one: 498, 31 and one:
+    // 55; 64 of 2547, the same bytes: 55), 300 x 1 x 8 with one of 30000 288 us (256: 20).
     pl.target = p.batch <= kSplitBatch && all < resident ? resident : 0;
     // workgroups: whole rounds of eight XCDs (find_job); jobs, and partials, are `target` at most
     const long long pairs = pl.target ? pl.target / pl.row_blocks : (long long)p.batch * c.kv_heads;
     pl.grid = (int)((pairs + 7) / 8 * 8 * pl.row_blocks);
     pl.late = pl.target && pl.slot_rows > kTicketRows;
     // A range more costs a partial written and read by every unit, at 4 TB/s, or a trip to memory for a chunk of sixteen; a
-    // tile of 64 keys takes (us, head_dim 128) 0.7 for up to 64 rows, 1.2 for 128, 2.2 for 256.
+    // tile of 64 keys takes (us, head_dim 128) 0.7 for up to 64 rows, 1.2 for 128, 2.2 for 256.  Over 14 shapes (1 to 500 rows a KV head, 700
+    // to 30000 keys) a quarter, half, twice and four times this cost take 1.09, 1.03, 1.02 and 1.12 of the time in the mean, and no shape
+    // is more than 13 % from its best of the five.
     const float tile = (pl.rows <= 64 ? 0.7f : pl.rows == 128 ? 1.2f : 2.2f) * (float)c.head_dim / 128.f;
     pl.apart = (pl.late ? (float)all * (float)pl.slot_rows * (float)c.head_dim * 8.f / 4e6f + 0.02f : 0.13f) / tile;
     const size_t jobs = (size_t)pl.target;
