@@ -190,3 +190,43 @@ def test_a_long_append_costs_what_its_pieces_cost():
             times.append(e[0].elapsed_time(e[1]))
         return min(times)
     assert best(calls[0]) < 2 * best(calls[1])
+
+
+def test_long_appends_in_a_graph():
+    """The two launches of a long append, captured once and replayed over other lengths, counts and table entries."""
+    import torch
+    from paper_2406_17276_amd import api
+    torch.manual_seed(4)
+    H, D, ps, B, most = 1, 64, 16, 2, 1700
+    n = 16 * 1600
+    caches = [api.alloc_paged_cache(B * most, H, ps, D, B, most) for _ in range(2)]
+    table = torch.randperm(B * most, device="cuda", dtype=torch.int32).view(B, most)
+    for c in caches:
+        c.k.zero_(), c.v.zero_()
+    K, V = (torch.randn(B, H, n, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    lens, count, new = P.i32([0, 0]), P.i32([n, n]), P.i32([0, 0])
+    call = lambda c, out: api.kv_append_paged(c, K, V, lens, count=count, new_len=out)
+    caches[0].table.copy_(table)
+    call(caches[0], new)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            call(caches[0], new)
+    for c in caches:
+        c.k.zero_(), c.v.zero_(), c.k_exp.fill_(127), c.v_exp.fill_(127)
+    for at, many, gap in (([0, 5], [n, n], None), ([1, 16 * 1690], [n, n], 1500), ([100, 0], [0, 3], None), ([7, 1600], [n, n - 1], 3), ([0, 0], [n, n], None)):
+        lens.copy_(P.i32(at)), count.copy_(P.i32(many))
+        for c in caches:
+            c.table.copy_(table)
+            if gap is not None:
+                c.table[0, gap] = -1
+        K.mul_(-0.75)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = call(caches[1], P.i32([-1, -1]))
+        assert torch.equal(new, eager), (at, many, gap)
+        for name in ("k", "v", "k_exp", "v_exp"):
+            assert torch.equal(getattr(caches[0], name), getattr(caches[1], name)), (name, at)
+    assert new.tolist() == [n, n]
